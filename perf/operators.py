@@ -234,7 +234,7 @@ def _handles(s):
     if c["kind"] != "norm":
         s["draft"] = tu.Draft(s["parents"])
     if "rows" in c:
-        s["ctx"] = tu.Context(c["rows"] + c["n"] + 3, device=DEV)
+        s["ctx"] = tu.Context(c["rows"] + c["n"], device=DEV)
         s["live"], s["cursor"] = [(260000, 260000 + c["rows"])], 260000 + c["rows"]
         s["ctx"].set_metadata(s["live"], s["cursor"])
     if c["kind"] == "attn":
@@ -244,11 +244,11 @@ def _handles(s):
         s["ws"] = torch.empty(tu.draft_verify_workspace_size(s["draft"], c["vocab"]), dtype=torch.uint8, device=DEV)
         s["result"] = torch.zeros(c["n"] + 2, dtype=torch.int32, device=DEV)
     if c["kind"] == "accept":
-        s["layers"] = [tu.LayerIO(tu.TU_LAYER_ATTN, None, None, None, None, k_cache=[s["kv"][0, l]], v_cache=[s["kv"][1, l]])
-                       for l in range(c["n_attn"])]
-        s["layers"] += [tu.LayerIO(tu.TU_LAYER_DELTA, None, s["k"][l], s["v"][l], None, state=[s["S"][l]],
-                                   beta=s["beta"][l], g=s["g"][l]) for l in range(c["n_delta"])]
-        s["convs"] = [(s["cs"][l], s["cx"][l]) for l in range(c["n_delta"])]
+        layers = [tu.LayerIO(tu.TU_LAYER_ATTN, None, None, None, None, k_cache=[s["kv"][0, l]], v_cache=[s["kv"][1, l]])
+                  for l in range(c["n_attn"])]
+        layers += [tu.LayerIO(tu.TU_LAYER_DELTA, None, s["k"][l], s["v"][l], None, state=[s["S"][l]],
+                              beta=s["beta"][l], g=s["g"][l]) for l in range(c["n_delta"])]
+        s["stack"] = tu.DraftStack(layers, s["attn"], s["delta"], [(s["cs"][l], s["cx"][l]) for l in range(c["n_delta"])])
 
 
 # ----------------------------------------------------------------------------- one pass
@@ -284,7 +284,7 @@ def _own(s):
                         workspace=s["ws"])
         return s["result"]
     s["ctx"].set_metadata(s["live"], s["cursor"])   # every pass keeps the path at the same length
-    tu.draft_accept(s["ctx"], s["draft"], s["path"], s["layers"], s["attn"], s["delta"], convs=s["convs"])
+    tu.draft_accept(s["ctx"], s["draft"], s["path"], s["stack"])
     return _kept(s)
 
 
