@@ -48,7 +48,7 @@
 extern "C" {
 #endif
 
-#define TU_ABI_VERSION 5
+#define TU_ABI_VERSION 6
 
 #define TU_OK 0
 #define TU_ERR_ARG (-1)       /* null pointer, unsupported or inconsistent shape */
@@ -140,8 +140,8 @@ const char* tu_last_error(void);
  * rounded to f16 must be finite (see the input range above). A failed check does not
  * stop the call (moves follow the host's spans and stay in bounds): it sets a bit in
  * the status the call keeps in the first 256 bytes of its workspace (compact_kv,
- * tail_prefill_attention, delta_rule_continue, refresh_vt_cache and
- * update_layer_stack). Each call is numbered, the bits carry its number and its
+ * tail_prefill_attention, delta_rule_continue, refresh_vt_cache,
+ * update_layer_stack, draft_attention and draft_verify). Each call is numbered, the bits carry its number and its
  * kernels record it, so the status never needs clearing and never shows bits of an
  * earlier call (a call with nothing to enqueue, T = 0, leaves it as it was):
  *   TU_FAULT_POSITIONS  d_pos disagrees with the host metadata (`live`, `len`), so
@@ -478,6 +478,153 @@ int attention_tv_distance(const float* p, const float* q, const int32_t* q_row_o
                           void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Speculative decoding. A drafter proposes a tree of tokens that continue a context; the
+ * model runs all of them in one pass (draft_append, draft_attention, draft_short_conv,
+ * draft_delta_rule), draft_verify accepts one path of the tree from the target's
+ * probabilities, and draft_accept keeps that path. Until then nothing of the context
+ * changes: the nodes' keys and values lie in cache rows [len, len + n), which no other
+ * call reads, and the carried states stay as they are. A tree of one node is ordinary
+ * decoding of one token.
+ *
+ * Node i continues node parent[i] < i, or the context itself (parent[i] == -1); it sees
+ * the context, its ancestors and itself, and has the position next_pos + its depth. The
+ * array is read during the call only.
+ */
+#define TU_MAX_DRAFT 128
+typedef struct tu_draft {
+  int32_t n;               /* nodes, 0 .. TU_MAX_DRAFT (0: nothing to do) */
+  const int32_t* parent;   /* host array [n] */
+} tu_draft;
+
+/*
+ * Norms of queries and keys for each head, and the rotation of the normed rows, in one pass:
+ *   TU_NORM_NONE  y = x
+ *   TU_NORM_RMS   y = x / sqrt(mean(x^2) + eps) * (weight + weight_offset)
+ *   TU_NORM_L2    y = x / sqrt(sum(x^2) + eps)
+ * then the pairs (j, j + rotary_dim/2) of y turn by position * rope_theta^(-2j/rotary_dim),
+ * the angle reduced in float64. Everything between the bf16 input and the bf16 output
+ * (nearest even) is held in fp32 or float64.
+ *  q_weight, k_weight: device bf16 [head_dim], shared by the heads; NULL stands for weights
+ *  of 1 (without offset). Only TU_NORM_RMS reads them. weight_offset 1 serves weights stored
+ *  as their difference from 1.
+ */
+#define TU_NORM_NONE 0
+#define TU_NORM_RMS 1
+#define TU_NORM_L2 2
+typedef struct tu_qk_norm {
+  int32_t kind;
+  float eps;               /* finite, >= 0 */
+  float weight_offset;     /* finite */
+  const void* q_weight;
+  const void* k_weight;
+} tu_qk_norm;
+
+/*
+ * The queries and keys of T tokens: token t's heads are consecutive rows of head_dim
+ * elements at q + t * q_stride (k alike); strides in elements, multiples of 8, at least
+ * heads * head_dim (unless T == 1). q or k may be NULL (with its output).
+ *  pos: optional device int32 [T], the tokens' positions; NULL: first_pos + t, below 2^31.
+ *  q_out, k_out: may be the inputs themselves (same stride); no other overlap.
+ * p gives the head counts, head_dim, rotary_dim and rope_theta. A normed and rotated tail
+ * goes through tail_prefill_attention with rotary_dim 0; TU_NORM_L2 with rotary_dim 0 norms
+ * the delta rule's queries and keys. Needs no workspace.
+ */
+int qk_norm_rope(const tu_attn_params* p, const tu_qk_norm* norm, const void* q, int64_t q_stride, const void* k,
+                 int64_t k_stride, int64_t T, int64_t first_pos, const int32_t* pos, void* q_out, int64_t q_out_stride,
+                 void* k_out, int64_t k_out_stride, void* stream);
+
+/*
+ * The nodes of a draft enter one attention layer: qk_norm_rope at the positions next_pos +
+ * depth, the queries into q_hat (device bf16 [n][n_q_heads][head_dim]), the keys and the
+ * values (v as they are, strided like k) into cache rows [len, len + n). norm NULL: none.
+ * d_pos and the metadata stay as they are.
+ */
+int draft_append(const tu_seq* seq, void* k_cache, void* v_cache, const tu_attn_params* p, const tu_qk_norm* norm,
+                 const tu_draft* draft, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const void* v, int64_t v_stride, void* q_hat, void* stream);
+
+/*
+ * Attention of a draft over the cache: node i attends to cache rows 0 .. len - 1 and to the
+ * rows len + j of its ancestors j and itself (their keys and values written by
+ * draft_append).
+ *  q_hat: device bf16 [n][n_q_heads][head_dim], normed and rotated;
+ *  out:   device bf16 [n][n_q_heads][head_dim], what the output projection reads (softmax
+ *         and sums in fp32, one rounding to bf16 at the end).
+ * Values are read as f16 (see the input range above; TU_FAULT_RANGE). p->kv_splits as in
+ * tail_prefill_attention.
+ */
+size_t draft_attention_workspace_size(const tu_attn_params* p, int32_t n, int64_t len);
+int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache, const tu_attn_params* p,
+                    const tu_draft* draft, const void* q_hat, void* out, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * The short convolutions of recurrent layers over a draft: the tap before a node's own row
+ * is its parent's row, and so on up the path, then the carried rows, newest first. The
+ * tensors are those of short_conv_continue_batch with T == draft->n; their states are only
+ * read.
+ */
+int draft_short_conv(const tu_draft* draft, const tu_conv_tensor* tensors, int32_t n, int32_t width,
+                     int32_t activation, void* stream);
+
+/*
+ * The gated delta rule of one layer over a draft: o_i is the output of delta_rule_continue
+ * for node i after its ancestors in order, from the carried state, which is only read.
+ * With u_i = beta_i (v_i - gamma_i S k_i) - sum over ancestors j of
+ * beta_i (gamma_i / gamma_j) (k_i . k_j) u_j (gamma: product of the gates along the path)
+ *   o_i = scale (gamma_i S q_i + sum over ancestors and i of (gamma_i / gamma_j) (q_i . k_j) u_j).
+ * Tensors as in delta_rule_continue with T == n; everything is held in fp32 (or products of
+ * three bf16 terms that carry as many bits). p->chunk is not used. Needs no workspace.
+ */
+int draft_delta_rule(const float* state, const void* q, const void* k, const void* v, const float* beta,
+                     const float* g, const tu_delta_params* p, const tu_draft* draft, float* out, void* stream);
+
+/*
+ * Verification of a draft. Node 0 is the only root and a token of the context already (it
+ * is always accepted); row i of `target` is the target's distribution behind node i.
+ * The children of the last accepted node m are tried in index order, child c with token x
+ * and random number u[c]:
+ *  with proposals (row m of `proposal` is the distribution the children of m were drawn
+ *  from), p and q being rows m, and b = 0, F = 1 at first: c is accepted if
+ *      u[c] * q(x) * F < max(p(x) - b q(x), 0),
+ *  else b becomes b + F and F = sum_t max(p(t) - b q(t), 0) (recursive rejection sampling:
+ *  the first test is u q < p, what is left after each is max(p - q, 0), normalised);
+ *  without (proposal NULL: distinct tokens the drafter chose), c is accepted if
+ *      u[c] * F < p(x),
+ *  else p(x) becomes 0 and F = sum_t p(t).
+ * With no child left the next token is drawn from what is left of row m: the smallest t
+ * whose cumulative sum exceeds u[0] times the whole (from row m of `target` itself if
+ * nothing is left, and -1 if that has no positive finite sum). Tests and sums are float64.
+ *  target, proposal: device fp32 [n] rows of `vocab` values, non-negative, row strides in
+ *            elements (at least vocab); tokens: device int32 [n] (a token outside [0, vocab)
+ *            is never accepted; tokens[0] is not read); u: device fp32 [n] in [0, 1).
+ *  result:   device int32 [n + 2]: accepted nodes (at least 1), the next token, then the
+ *            accepted path from node 0 on, filled up with -1.
+ */
+size_t draft_verify_workspace_size(int32_t n, int64_t vocab);
+int draft_verify(const tu_draft* draft, const int32_t* tokens, const float* target, int64_t target_stride,
+                 const float* proposal, int64_t proposal_stride, int64_t vocab, const float* u, int32_t* result,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Keeps an accepted path of the draft in a layer stack. path: host int32 [n_path] node
+ * indices, the first one a root, each later one a child of the one before.
+ *  attention layers (k_cache[0], v_cache[0] of one context): cache rows len + path[j]
+ *    move to len + j; d_pos gets their positions;
+ *  delta layers: state[0] takes the path's tokens in order (k, v, beta, g hold the draft's
+ *    n rows; q and out are not used), in fp32, as delta_rule_continue does token by token;
+ *  conv (n_conv tensors of the common width, weight and out not used): the carried rows
+ *    become the last width - 1 of the carried rows followed by the path's rows of x.
+ * Then len and next_pos grow by n_path and the live positions by [next_pos, next_pos +
+ * n_path); vt_rows stays (the V^T copies take the new rows with the next refresh).
+ * attn may be NULL without attention layers, delta without delta layers. n_path 0 changes
+ * nothing. Needs no workspace.
+ */
+int draft_accept(tu_seq* seq, const tu_draft* draft, const int32_t* path, int32_t n_path, const tu_layer_io* layers,
+                 int32_t n_layers, const tu_attn_params* attn, const tu_delta_params* delta, const tu_conv_tensor* conv,
+                 int32_t n_conv, int32_t width, void* stream);
+
+/*
  * Kernel timing (diagnostics, not part of the update). While enabled for the
  * calling thread, every kernel the library launches is bracketed by two HIP
  * events recorded on the launch's stream. tu_profile_collect waits for those
@@ -487,7 +634,8 @@ int attention_tv_distance(const float* p, const float* q, const int32_t* q_row_o
  * (or a negative status) and clears the records. Names (one per launch or pair
  * of launches): compact (keep-scan, then gather), rope_vt_pack (RoPE + append of
  * the tail with the V^T packing of the key tiles), attention, attention_merge,
- * delta_prep, delta_chain or delta_chain_direct, delta_step, short_conv, relocate, probe, group_mass, tv_distance.
+ * delta_prep, delta_chain or delta_chain_direct, delta_step, short_conv, relocate, probe, group_mass, tv_distance,
+ * qk_norm_rope (also draft_append), draft_attention, draft_merge, draft_conv, draft_delta, draft_verify, draft_accept.
  */
 int tu_profile_enable(int on);
 int tu_profile_collect(char* names, int32_t name_stride, int32_t* counts, double* total_ms, int32_t max_entries);

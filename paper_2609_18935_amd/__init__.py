@@ -8,11 +8,18 @@ It also continues the recurrent layers' short convolution from its carried state
 and provides the slot-preserving and tail-and-relocate placements the paper compares
 (Section 5.2) together with the relocation of stored keys, and the attention
 diagnostics of Section 5.3 (probe distributions, group masses, total variation).
+A context also decodes speculatively: a tree of drafted tokens runs through both kinds of
+layer in one pass (queries and keys normed for each head and rotated, attention over the
+cache and each node's ancestors, the recurrent layers along each node's path), is verified
+against the target's probabilities, and the accepted path is kept.
 `binding` is the ctypes layer over its C ABI (include/tailupdate.h).
 """
 from .binding import (  # noqa: F401
     Context,
+    Draft,
+    DraftStack,
     LayerIO,
+    QkNorm,
     StackUpdate,
     TailUpdateError,
     attention_group_mass,
@@ -24,12 +31,21 @@ from .binding import (  # noqa: F401
     compact_kv_noalloc,
     delta_params,
     delta_rule_continue,
+    draft_accept,
+    draft_append,
+    draft_attention,
+    draft_attention_workspace_size,
+    draft_delta_rule,
+    draft_short_conv,
+    draft_verify,
+    draft_verify_workspace_size,
     new_vt_cache,
     vt_cache_bytes,
     workspace_faults,
     lib,
     profile_collect,
     profile_enable,
+    qk_norm_rope,
     refresh_vt_cache,
     relocate_keys,
     short_conv_continue,

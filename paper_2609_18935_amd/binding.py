@@ -76,6 +76,14 @@ class tu_conv_tensor(ctypes.Structure):
                 ("reserved", _i32)]
 
 
+class tu_draft(ctypes.Structure):
+    _fields_ = [("n", _i32), ("parent", ctypes.POINTER(_i32))]
+
+
+class tu_qk_norm(ctypes.Structure):
+    _fields_ = [("kind", _i32), ("eps", _f32), ("weight_offset", _f32), ("q_weight", _vp), ("k_weight", _vp)]
+
+
 class tu_update(ctypes.Structure):
     _fields_ = [("n_seq", _i32), ("seqs", ctypes.POINTER(tu_seq_update)), ("n_layers", _i32),
                 ("layers", ctypes.POINTER(tu_layer_io)), ("attn", tu_attn_params), ("delta", tu_delta_params)]
@@ -116,6 +124,22 @@ _SIGNATURES = {
                                     _vp, ctypes.c_size_t, _vp]),
     "attention_tv_workspace_size": (ctypes.c_size_t, [_i64]),
     "attention_tv_distance": (_i32, [_vp, _vp, _vp, _i64, _vp, _vp, ctypes.c_size_t, _vp]),
+    "qk_norm_rope": (_i32, [ctypes.POINTER(tu_attn_params), ctypes.POINTER(tu_qk_norm), _vp, _i64, _vp, _i64, _i64, _i64,
+                            _vp, _vp, _i64, _vp, _i64, _vp]),
+    "draft_append": (_i32, [ctypes.POINTER(tu_seq), _vp, _vp, ctypes.POINTER(tu_attn_params), ctypes.POINTER(tu_qk_norm),
+                            ctypes.POINTER(tu_draft), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "draft_attention_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(tu_attn_params), _i32, _i64]),
+    "draft_attention": (_i32, [ctypes.POINTER(tu_seq), _vp, _vp, ctypes.POINTER(tu_attn_params),
+                               ctypes.POINTER(tu_draft), _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "draft_short_conv": (_i32, [ctypes.POINTER(tu_draft), ctypes.POINTER(tu_conv_tensor), _i32, _i32, _i32, _vp]),
+    "draft_delta_rule": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(tu_delta_params),
+                                ctypes.POINTER(tu_draft), _vp, _vp]),
+    "draft_verify_workspace_size": (ctypes.c_size_t, [_i32, _i64]),
+    "draft_verify": (_i32, [ctypes.POINTER(tu_draft), _vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, ctypes.c_size_t,
+                            _vp]),
+    "draft_accept": (_i32, [ctypes.POINTER(tu_seq), ctypes.POINTER(tu_draft), ctypes.POINTER(_i32), _i32,
+                            ctypes.POINTER(tu_layer_io), _i32, ctypes.POINTER(tu_attn_params),
+                            ctypes.POINTER(tu_delta_params), ctypes.POINTER(tu_conv_tensor), _i32, _i32, _vp]),
     "tu_workspace_faults": (_i32, [_vp, ctypes.POINTER(_i32), _vp]),
     "tu_profile_enable": (_i32, [_i32]),
     "tu_profile_collect": (_i32, [ctypes.c_char_p, _i32, ctypes.POINTER(_i32), ctypes.POINTER(ctypes.c_double),
@@ -123,7 +147,7 @@ _SIGNATURES = {
 }
 
 _lib_handle = None
-ABI_VERSION = 5   # TU_ABI_VERSION of include/tailupdate.h that these structures follow
+ABI_VERSION = 6   # TU_ABI_VERSION of include/tailupdate.h that these structures follow
 
 
 def lib():
@@ -509,6 +533,283 @@ class StackUpdate:
 
     def run(self, workspace: torch.Tensor, stream=None):
         _check(lib().update_layer_stack(ctypes.byref(self.u), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- speculative decoding
+
+TU_MAX_DRAFT = 128
+TU_NORM_NONE = 0
+TU_NORM_RMS = 1
+TU_NORM_L2 = 2
+_NORMS = {"none": TU_NORM_NONE, "rms": TU_NORM_RMS, "l2": TU_NORM_L2}
+_ACTIVATIONS = {"silu": TU_CONV_SILU, "none": TU_CONV_IDENTITY}
+
+
+def _need(t: torch.Tensor, what: str, dtype, shape, device, strided: int = 0) -> int:
+    """The tensor's address, once it is what a kernel will take it for: dtype, shape (None: not checked), device
+    of the call, contiguous (strided: the first `strided` dimensions may have strides of their own)."""
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} must be {dtype}, is {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the call is for {device}")
+    if strided:
+        inner = 1
+        for d in range(t.dim() - 1, strided - 1, -1):
+            if t.shape[d] != 1 and t.stride(d) != inner:
+                raise ValueError(f"the rows of {what} must be contiguous")
+            inner *= t.shape[d]
+    elif not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def _call_device(t: torch.Tensor) -> torch.device:
+    """The device a call runs on: that of its first tensor, which has to be the current one."""
+    d = t.device
+    if d.type == "cuda":
+        if d.index != torch.cuda.current_device():
+            raise ValueError(f"tensors on {d}, the current device is cuda:{torch.cuda.current_device()}")
+    elif torch.cuda.is_available():
+        raise ValueError(f"tensors must be on the GPU, not on {d}")
+    return d
+
+
+class Draft:
+    """A tree of drafted tokens: parents[i] < i is the node that node i continues, -1 the context."""
+
+    def __init__(self, parents: Sequence[int]):
+        self.parents = [int(p) for p in parents]
+        self.n = len(self.parents)
+        self._parent = (_i32 * max(1, self.n))(*self.parents)
+        self.c = tu_draft(self.n, self._parent)
+        self._ref = ctypes.byref(self.c)
+
+
+class QkNorm:
+    """Norm of queries and keys for each head: "none", "rms" (weights bf16 [head_dim] or None, multiplied as
+    weight + offset) or "l2"."""
+
+    def __init__(self, kind: str = "rms", eps: float = 1e-6, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, weight_offset: float = 0.0):
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dtype is not torch.bfloat16 or w.dim() != 1):
+                raise ValueError("norm weights are bf16 vectors of head_dim values")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.c = tu_qk_norm(_NORMS[kind], float(eps), float(weight_offset), _ptr(q_weight), _ptr(k_weight))
+        self._ref = ctypes.byref(self.c)
+
+    def _of(self, head_dim: int, device):
+        for w in (self.q_weight, self.k_weight):
+            if w is not None:
+                _need(w, "norm weight", torch.bfloat16, (head_dim,), device)
+        return self._ref
+
+
+def qk_norm_rope(params: tu_attn_params, q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                 q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], norm: Optional[QkNorm] = None,
+                 first_pos: int = 0, positions: Optional[torch.Tensor] = None, stream=None):
+    """Norms and rotates the heads of q [T][Hq][D] and k [T][Hkv][D] (either may be None) into q_out and k_out; a
+    token's heads are contiguous, tokens may lie apart. positions: int32 [T] on the device, else first_pos + t."""
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("neither queries nor keys")
+    dev, T, D = _call_device(first), int(first.shape[0]), params.head_dim
+    args = []
+    for x, y, what, heads in ((q, q_out, "q", params.n_q_heads), (k, k_out, "k", params.n_kv_heads)):
+        if x is None:
+            args.append((None, 0, None, 0))
+            continue
+        shape = (T, heads, D)
+        args.append((_need(x, what, torch.bfloat16, shape, dev, 1), x.stride(0),
+                     _need(y, what + "_out", torch.bfloat16, shape, dev, 1), y.stride(0)))
+    (qp, qs, qo, qos), (kp, ks, ko, kos) = args
+    pos = None if positions is None else _need(positions, "positions", torch.int32, (T,), dev)
+    _check(lib().qk_norm_rope(ctypes.byref(params), None if norm is None else norm._of(D, dev), qp, qs, kp, ks, T,
+                              int(first_pos), pos, qo, qos, ko, kos, _stream(stream)))
+
+
+def _check_caches(ctx: "Context", k_cache, v_cache, params, dev):
+    """Addresses of the caches, which must hold every row of the context's capacity."""
+    Hkv, D = params.n_kv_heads, params.head_dim
+    for c, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if c.dim() != 3 or c.shape[0] < ctx.c.capacity or c.shape[1] != Hkv or c.shape[2] != D:
+            raise ValueError(f"{what} must be [>= {ctx.capacity}][{Hkv}][{D}], is {tuple(c.shape)}")
+    return _need(k_cache, "k_cache", torch.bfloat16, None, dev), _need(v_cache, "v_cache", torch.bfloat16, None, dev)
+
+
+def draft_append(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, params: tu_attn_params, draft: Draft,
+                 q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_hat: torch.Tensor,
+                 norm: Optional[QkNorm] = None, stream=None):
+    """The nodes' queries (into q_hat [n][Hq][D]), keys and values (into cache rows [len, len + n)) enter one
+    attention layer, normed and rotated at the positions cursor + depth."""
+    dev, n, D = _call_device(q_hat), draft.n, params.head_dim
+    kc, vc = _check_caches(ctx, k_cache, v_cache, params, dev)
+    kv = (n, params.n_kv_heads, D)
+    bf = torch.bfloat16
+    _check(lib().draft_append(ctypes.byref(ctx.c), kc, vc, ctypes.byref(params),
+                              None if norm is None else norm._of(D, dev), draft._ref,
+                              _need(q, "q", bf, (n, params.n_q_heads, D), dev, 1), q.stride(0) if n else 0,
+                              _need(k, "k", bf, kv, dev, 1), k.stride(0) if n else 0,
+                              _need(v, "v", bf, kv, dev, 1), v.stride(0) if n else 0,
+                              _need(q_hat, "q_hat", bf, (n, params.n_q_heads, D), dev), _stream(stream)))
+
+
+def draft_attention_workspace_size(ctx: Context, params: tu_attn_params, draft: Draft) -> int:
+    return int(lib().draft_attention_workspace_size(ctypes.byref(params), draft.n, ctx.len))
+
+
+def draft_attention(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, params: tu_attn_params, draft: Draft,
+                    q_hat: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """out [n][Hq][D] (bf16): each node attends to the cache, its ancestors and itself. Returns the workspace."""
+    dev = _call_device(q_hat)
+    kc, vc = _check_caches(ctx, k_cache, v_cache, params, dev)
+    shape = (draft.n, params.n_q_heads, params.head_dim)
+    qp = _need(q_hat, "q_hat", torch.bfloat16, shape, dev)
+    op = _need(out, "out", torch.bfloat16, shape, dev)
+    if workspace is None:
+        workspace = _workspace(draft_attention_workspace_size(ctx, params, draft), dev, None, stream)
+    _check(lib().draft_attention(ctypes.byref(ctx.c), kc, vc, ctypes.byref(params), draft._ref, qp, op,
+                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return workspace
+
+
+def draft_short_conv(draft: Draft, items, activation: str = "silu", stream=None):
+    """items: sequence of (state [W-1][C], x [n][C], weight [C][W], out [n][C]) bf16 tensors sharing one width: the
+    convolution along each node's path, the states only read."""
+    arr = (tu_conv_tensor * max(1, len(items)))()
+    W, bf = None, torch.bfloat16
+    for i, (st, x, w, out) in enumerate(items):
+        dev = _call_device(x)
+        C = int(x.shape[1])
+        if W is not None and w.shape[1] != W:
+            raise ValueError("all tensors of a batch share one width")
+        W = int(w.shape[1])
+        rows = (draft.n, C)
+        t = arr[i]
+        t.state = None if st is None else _need(st, "state", bf, (W - 1, C), dev)
+        t.x, t.weight = _need(x, "x", bf, rows, dev), _need(w, "weight", bf, (C, W), dev)
+        t.out, t.T, t.channels = _need(out, "out", bf, rows, dev), draft.n, C
+    _check(lib().draft_short_conv(draft._ref, arr, len(items), W or 1, _ACTIVATIONS[activation], _stream(stream)))
+
+
+def draft_delta_rule(state: torch.Tensor, q, k, v, beta, g, params: tu_delta_params, draft: Draft, out: torch.Tensor,
+                     stream=None):
+    """out [n][Hv][d_v] (fp32): the gated delta rule along each node's path from `state`, which is only read."""
+    dev, n = _call_device(state), draft.n
+    Hk, Hv, d = params.n_k_heads, params.n_v_heads, params.d_k
+    bf, f32 = torch.bfloat16, torch.float32
+    _check(lib().draft_delta_rule(_need(state, "state", f32, (Hv, d, d), dev), _need(q, "q", bf, (n, Hk, d), dev),
+                                  _need(k, "k", bf, (n, Hk, d), dev), _need(v, "v", bf, (n, Hv, d), dev),
+                                  _need(beta, "beta", f32, (n, Hv), dev), _need(g, "g", f32, (n, Hv), dev),
+                                  ctypes.byref(params), draft._ref, _need(out, "out", f32, (n, Hv, d), dev),
+                                  _stream(stream)))
+
+
+def draft_verify_workspace_size(draft: Draft, vocab: int) -> int:
+    return int(lib().draft_verify_workspace_size(draft.n, int(vocab)))
+
+
+def draft_verify(draft: Draft, tokens: torch.Tensor, target: torch.Tensor, uniforms: torch.Tensor,
+                 result: Optional[torch.Tensor] = None, proposal: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Accepts a path of the draft: tokens int32 [n], target and proposal fp32 [n][V] (rows may lie apart), uniforms
+    fp32 [n]. Returns result, int32 [n + 2]: accepted nodes, next token, the path filled up with -1."""
+    dev, n, V = _call_device(target), draft.n, int(target.shape[-1])
+    f32 = torch.float32
+    if result is None:
+        result = torch.empty(n + 2, dtype=torch.int32, device=dev)
+        ts = _torch_stream(stream, dev)
+        if ts is not None and ts != torch.cuda.current_stream(dev):
+            result.record_stream(ts)
+    if workspace is None:
+        workspace = _workspace(draft_verify_workspace_size(draft, V), dev, None, stream)
+    tp = _need(target, "target", f32, (n, V), dev, 1)
+    pp = None if proposal is None else _need(proposal, "proposal", f32, (n, V), dev, 1)
+    _check(lib().draft_verify(draft._ref, _need(tokens, "tokens", torch.int32, (n,), dev), tp,
+                              target.stride(0) if n > 1 else V, pp,
+                              0 if proposal is None else proposal.stride(0) if n > 1 else V, V,
+                              _need(uniforms, "uniforms", f32, (n,), dev),
+                              _need(result, "result", torch.int32, (n + 2,), dev), workspace.data_ptr(),
+                              workspace.numel() * workspace.element_size(), _stream(stream)))
+    return result
+
+
+class DraftStack:
+    """The layers and convolutions of a context that an accepted path is kept in (ctypes structs built once,
+    reusable as long as the tensors are the same): LayerIO of both kinds (caches, states and the draft's k, v,
+    beta, g) and convs, a sequence of (state [W-1][C], x [n][C]) with one width."""
+
+    def __init__(self, layers: Sequence[LayerIO], attn: Optional[tu_attn_params] = None,
+                 delta: Optional[tu_delta_params] = None, convs: Sequence = ()):
+        self.attn, self.delta, self._keep = attn, delta, [layers, convs]
+        bf, f32 = torch.bfloat16, torch.float32
+        self.device, self.rows, self.capacity, self.width = None, None, None, 1
+        tensors = [t for L in layers for t in ((L.k_cache or [None])[0], (L.state or [None])[0]) if t is not None]
+        tensors += [st for st, _ in convs]
+        if tensors:
+            self.device = tensors[0].device
+
+        def rows(t, what):
+            if self.rows is not None and t.shape[0] != self.rows:
+                raise ValueError(f"{what} has {t.shape[0]} rows, other tensors of the draft have {self.rows}")
+            self.rows = int(t.shape[0])
+
+        def one(t, what, dtype, shape):
+            a = (_vp * 1)(_need(t, what, dtype, shape, self.device))
+            self._keep.append(a)
+            return a
+
+        self._layers = (tu_layer_io * max(1, len(layers)))()
+        self.n_layers = len(layers)
+        for L, c in zip(layers, self._layers):
+            c.kind = L.kind
+            if L.kind == TU_LAYER_ATTN:
+                if attn is None:
+                    raise ValueError("attention layers need attn")
+                for t, what in ((L.k_cache[0], "k_cache"), (L.v_cache[0], "v_cache")):
+                    if t.dim() != 3 or t.shape[1] != attn.n_kv_heads or t.shape[2] != attn.head_dim:
+                        raise ValueError(f"{what} must be [capacity][{attn.n_kv_heads}][{attn.head_dim}]")
+                    self.capacity = min(t.shape[0], self.capacity or t.shape[0])
+                c.k_cache = one(L.k_cache[0], "k_cache", bf, None)
+                c.v_cache = one(L.v_cache[0], "v_cache", bf, None)
+            else:
+                if delta is None:
+                    raise ValueError("delta layers need delta")
+                Hk, Hv, d = delta.n_k_heads, delta.n_v_heads, delta.d_k
+                rows(L.k, "k")
+                c.state = one(L.state[0], "state", f32, (Hv, d, d))
+                c.k = _need(L.k, "k", bf, (self.rows, Hk, d), self.device)
+                c.v = _need(L.v, "v", bf, (self.rows, Hv, d), self.device)
+                c.beta = _need(L.beta, "beta", f32, (self.rows, Hv), self.device)
+                c.g = _need(L.g, "g", f32, (self.rows, Hv), self.device)
+        self._convs = (tu_conv_tensor * max(1, len(convs)))()
+        self.n_convs = len(convs)
+        for i, (st, x) in enumerate(convs):
+            if i and st.shape[0] + 1 != self.width:
+                raise ValueError("all convolutions share one width")
+            self.width = int(st.shape[0]) + 1
+            rows(x, "x")
+            c = self._convs[i]
+            c.state = _need(st, "state", bf, (self.width - 1, x.shape[1]), self.device)
+            c.x, c.T, c.channels = _need(x, "x", bf, (self.rows, x.shape[1]), self.device), self.rows, int(x.shape[1])
+
+
+def draft_accept(ctx: Context, draft: Draft, path: Sequence[int], stack: DraftStack, stream=None):
+    """Keeps the accepted path (node indices from a root on) in the stack's caches and states; the context
+    advances by its length."""
+    if stack.rows is not None and stack.rows != draft.n:
+        raise ValueError(f"the stack's tensors have {stack.rows} rows, the draft {draft.n} nodes")
+    if stack.capacity is not None and stack.capacity < ctx.c.capacity:
+        raise ValueError(f"a cache has {stack.capacity} rows, the context's capacity is {ctx.capacity}")
+    if _call_device(ctx.pos) != (stack.device or ctx.pos.device):
+        raise ValueError(f"the context is on {ctx.pos.device}, its layers on {stack.device}")
+    _check(lib().draft_accept(ctypes.byref(ctx.c), draft._ref, (_i32 * max(1, len(path)))(*path), len(path),
+                              stack._layers, stack.n_layers,
+                              None if stack.attn is None else ctypes.byref(stack.attn),
+                              None if stack.delta is None else ctypes.byref(stack.delta), stack._convs, stack.n_convs,
+                              stack.width, _stream(stream)))
 
 
 TU_FAULT_POSITIONS = 1   # device positions disagreed with the host's live runs

@@ -1,0 +1,160 @@
+// Launch records of the speculative decoding kernels (a tree of drafted tokens over one
+// context). Every kernel takes its record by value.
+#pragma once
+
+#include "common.h"
+
+namespace tu {
+
+constexpr int kMaxDraft = 128;   // TU_MAX_DRAFT
+
+// Bit j of the mask of node i: node i sees node j (an ancestor, or i itself).
+struct DraftMasks {
+  uint64_t m[kMaxDraft][2];
+};
+
+struct NormArgs {
+  const bf16_t* in[3];    // q, k, v (v is copied; draft_append only)
+  bf16_t* out[3];
+  int64_t in_stride[3];   // elements from one token to the next
+  int64_t out_stride[3];
+  const bf16_t* weight[2];  // of q, of k, or null
+  const int32_t* pos;     // positions, or null: first_pos + t, or first_pos + depth[t]
+  int64_t first_pos;
+  double turn_lane[16];   // theta^(-16 l / r) / (2 pi): turns per position of pair 8 l
+  double turn_elem[8];    // theta^(-2 e / r)
+  int32_t heads_end[3];   // prefix of the head counts of q, k, v
+  int32_t T;
+  int32_t kind;           // TU_NORM_*
+  int32_t rotary;
+  float eps;
+  float weight_offset;
+  int32_t per_group;      // heads of one lane group
+  int32_t n_groups;       // lane groups of a token
+  int32_t use_depth;
+  uint8_t depth[kMaxDraft];
+};
+
+struct DraftAttnArgs {
+  const bf16_t* q_hat;    // [n][Hq][D]
+  const bf16_t* k_cache;  // [>= len + n][Hkv][D]
+  const bf16_t* v_cache;
+  bf16_t* out;            // [n][Hq][D]
+  _Float16* part_o;       // [splits][n * Hq][D] normalised partial outputs (unused when n_splits == 1)
+  float* part_ml;         // [splits][n * Hq][2] reference max (log2 units), sum
+  CallStatus status;
+  int32_t len;
+  int32_t n;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t n_tiles;        // ceil(n * G / kDraftRows)
+  int32_t n_splits;
+  float scale_log2;       // softmax_scale * log2(e)
+  int32_t pad;
+  DraftMasks seen;
+};
+constexpr int kDraftRows = 256;         // packed query rows of an attention workgroup
+constexpr int kDraftStageBytes = 16384; // K (or V) bytes of one stage
+constexpr int draft_stage_keys(int D) { return kDraftStageBytes / (2 * D); }
+
+struct DraftConvArgs {
+  ConvJob job[kMaxConvJobs];   // state is only read
+  int32_t n_jobs;
+  int32_t n;                   // nodes
+  int32_t width;
+  int32_t pad;
+  int8_t up[kMaxDraft][8];     // row under the t-th tap back from node i: a node, or -1, -2, .. for the carried rows, newest first
+};
+
+struct DraftDeltaArgs {
+  const float* state;   // [Hv][d][d]
+  const bf16_t* q;      // [n][Hk][d]
+  const bf16_t* k;
+  const bf16_t* v;      // [n][Hv][d]
+  const float* beta;    // [n][Hv]
+  const float* g;
+  float* out;           // [n][Hv][d]
+  int32_t n;
+  int32_t n_k_heads;
+  int32_t n_v_heads;
+  int32_t rounds;       // pointer doublings that reach every root: 2^rounds > the deepest node's depth
+  float scale;
+  int16_t parent[kMaxDraft];
+  DraftMasks seen;
+};
+
+constexpr int kDrawThreads = 512;
+constexpr int kDrawPer = 8;       // row elements of a thread that stay in registers
+constexpr int kDrawMaxBlocks = 64;
+struct DraftVerifyArgs {
+  const int32_t* tokens;
+  const float* target;
+  const float* proposal;    // or null
+  const float* u;
+  int32_t* result;
+  int64_t target_stride;
+  int64_t proposal_stride;
+  int64_t vocab;
+  int32_t* arrived;         // [kMaxDraft + 1] workgroups that have written their part of a pass
+  double* part;             // [kMaxDraft + 1][kDrawMaxBlocks] partial sums
+  CallStatus status;
+  int32_t n;
+  int32_t n_blocks;         // workgroups of a pass, each a contiguous slice of the row
+  int64_t slice;            // elements of a slice
+  int16_t parent[kMaxDraft];
+  DraftMasks seen;
+};
+
+constexpr int kMaxAcceptDelta = 32;
+constexpr int kMaxAcceptConv = 32;
+constexpr int kMaxAcceptBufs = 32;
+struct AcceptDelta {
+  float* state;
+  const bf16_t* k;
+  const bf16_t* v;
+  const float* beta;
+  const float* g;
+};
+struct AcceptConv {
+  bf16_t* state;
+  const bf16_t* x;
+  int32_t channels;
+  int32_t block_begin;
+};
+struct AcceptArgs {
+  AcceptDelta delta[kMaxAcceptDelta];
+  AcceptConv conv[kMaxAcceptConv];
+  bf16_t* bufs[kMaxAcceptBufs];   // K and V caches
+  int32_t* pos;                   // d_pos, or null
+  int64_t len;
+  int64_t next_pos;
+  int32_t n_delta;
+  int32_t n_conv;
+  int32_t n_bufs;
+  int32_t row_chunks;             // 16-byte chunks of a cache row
+  int32_t n_k_heads;
+  int32_t n_v_heads;
+  int32_t d;
+  int32_t width;
+  int32_t n_path;
+  int32_t delta_blocks;           // workgroups of the three parts
+  int32_t conv_blocks;
+  int32_t row_blocks;             // per buffer
+  uint8_t path[kMaxDraft];
+};
+
+hipError_t launch_qk_norm(const NormArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_draft_attention(const DraftAttnArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_draft_merge(const DraftAttnArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_draft_conv(DraftConvArgs& a, hipStream_t s);   // sets each job's block_begin, n_cblocks
+hipError_t launch_draft_delta(const DraftDeltaArgs& a, int d, hipStream_t s);
+hipError_t launch_draft_clear(const DraftVerifyArgs& a, hipStream_t s);
+hipError_t launch_draft_draw(const DraftVerifyArgs& a, hipStream_t s);
+hipError_t launch_draft_accept(AcceptArgs& a, hipStream_t s);    // sets the block counts
+
+static_assert(sizeof(NormArgs) <= kMaxKernargBytes && sizeof(DraftAttnArgs) <= kMaxKernargBytes &&
+                  sizeof(DraftConvArgs) <= kMaxKernargBytes && sizeof(DraftDeltaArgs) <= kMaxKernargBytes &&
+                  sizeof(DraftVerifyArgs) <= kMaxKernargBytes && sizeof(AcceptArgs) <= kMaxKernargBytes,
+              "draft launch records");
+
+}  // namespace tu
