@@ -545,35 +545,51 @@ _NORMS = {"none": TU_NORM_NONE, "rms": TU_NORM_RMS, "l2": TU_NORM_L2}
 _ACTIVATIONS = {"silu": TU_CONV_SILU, "none": TU_CONV_IDENTITY}
 
 
-def _need(t: torch.Tensor, what: str, dtype, shape, device, strided: int = 0) -> int:
+def _need(t: torch.Tensor, what: str, dtype, shape, device: int, strided: bool = False) -> int:
     """The tensor's address, once it is what a kernel will take it for: dtype, shape (None: not checked), device
-    of the call, contiguous (strided: the first `strided` dimensions may have strides of their own)."""
+    of the call (-1: host, for the checks alone), contiguous (strided: tokens may lie apart)."""
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype}, is {t.dtype}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, has {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{what} is on {t.device}, the call is for {device}")
-    if strided:
-        inner = 1
-        for d in range(t.dim() - 1, strided - 1, -1):
-            if t.shape[d] != 1 and t.stride(d) != inner:
-                raise ValueError(f"the rows of {what} must be contiguous")
-            inner *= t.shape[d]
-    elif not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return t.data_ptr()
+    if t.get_device() != device:
+        raise ValueError(f"{what} is on {t.device}, the call is for {'cuda:%d' % device if device >= 0 else 'cpu'}")
+    inner = 1
+    for d in range(t.dim() - 1, 0, -1):
+        if t.shape[d] != 1 and t.stride(d) != inner:
+            break
+        inner *= t.shape[d]
+    else:
+        if strided:
+            return t.data_ptr()
+    raise ValueError(f"the rows of {what} must be contiguous" if strided else f"{what} must be contiguous")
 
 
-def _call_device(t: torch.Tensor) -> torch.device:
-    """The device a call runs on: that of its first tensor, which has to be the current one."""
-    d = t.device
-    if d.type == "cuda":
-        if d.index != torch.cuda.current_device():
-            raise ValueError(f"tensors on {d}, the current device is cuda:{torch.cuda.current_device()}")
+def _call_device(t: torch.Tensor) -> int:
+    """The device a call runs on: that of its first tensor, which has to be the current one (-1: host tensors,
+    without a GPU, for the checks alone)."""
+    d = t.get_device()
+    if d >= 0:
+        if d != torch._C._cuda_getDevice():
+            raise ValueError(f"tensors on cuda:{d}, the current device is cuda:{torch.cuda.current_device()}")
     elif torch.cuda.is_available():
-        raise ValueError(f"tensors must be on the GPU, not on {d}")
+        raise ValueError(f"tensors must be on the GPU, not on {t.device}")
     return d
+
+
+def _stream_on(stream, device: int) -> Optional[int]:
+    """_stream for a call whose device is known to be the current one."""
+    if stream is None and device >= 0 and _raw_stream:
+        return _raw_stream(device)
+    return _stream(stream)
+
+
+def _workspace_of(workspace: torch.Tensor, device: int) -> tuple:
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and on the call's device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 class Draft:
@@ -600,7 +616,7 @@ class QkNorm:
         self.c = tu_qk_norm(_NORMS[kind], float(eps), float(weight_offset), _ptr(q_weight), _ptr(k_weight))
         self._ref = ctypes.byref(self.c)
 
-    def _of(self, head_dim: int, device):
+    def _of(self, head_dim: int, device: int):
         for w in (self.q_weight, self.k_weight):
             if w is not None:
                 _need(w, "norm weight", torch.bfloat16, (head_dim,), device)
@@ -615,19 +631,19 @@ def qk_norm_rope(params: tu_attn_params, q: Optional[torch.Tensor], k: Optional[
     first = q if q is not None else k
     if first is None:
         raise ValueError("neither queries nor keys")
-    dev, T, D = _call_device(first), int(first.shape[0]), params.head_dim
+    dev, T, D = _call_device(first), first.shape[0], params.head_dim
     args = []
     for x, y, what, heads in ((q, q_out, "q", params.n_q_heads), (k, k_out, "k", params.n_kv_heads)):
         if x is None:
             args.append((None, 0, None, 0))
             continue
         shape = (T, heads, D)
-        args.append((_need(x, what, torch.bfloat16, shape, dev, 1), x.stride(0),
-                     _need(y, what + "_out", torch.bfloat16, shape, dev, 1), y.stride(0)))
+        args.append((_need(x, what, torch.bfloat16, shape, dev, True), x.stride(0),
+                     _need(y, what + "_out", torch.bfloat16, shape, dev, True), y.stride(0)))
     (qp, qs, qo, qos), (kp, ks, ko, kos) = args
     pos = None if positions is None else _need(positions, "positions", torch.int32, (T,), dev)
     _check(lib().qk_norm_rope(ctypes.byref(params), None if norm is None else norm._of(D, dev), qp, qs, kp, ks, T,
-                              int(first_pos), pos, qo, qos, ko, kos, _stream(stream)))
+                              int(first_pos), pos, qo, qos, ko, kos, _stream_on(stream, dev)))
 
 
 def _check_caches(ctx: "Context", k_cache, v_cache, params, dev):
@@ -650,10 +666,10 @@ def draft_append(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, par
     bf = torch.bfloat16
     _check(lib().draft_append(ctypes.byref(ctx.c), kc, vc, ctypes.byref(params),
                               None if norm is None else norm._of(D, dev), draft._ref,
-                              _need(q, "q", bf, (n, params.n_q_heads, D), dev, 1), q.stride(0) if n else 0,
-                              _need(k, "k", bf, kv, dev, 1), k.stride(0) if n else 0,
-                              _need(v, "v", bf, kv, dev, 1), v.stride(0) if n else 0,
-                              _need(q_hat, "q_hat", bf, (n, params.n_q_heads, D), dev), _stream(stream)))
+                              _need(q, "q", bf, (n, params.n_q_heads, D), dev, True), q.stride(0) if n else 0,
+                              _need(k, "k", bf, kv, dev, True), k.stride(0) if n else 0,
+                              _need(v, "v", bf, kv, dev, True), v.stride(0) if n else 0,
+                              _need(q_hat, "q_hat", bf, (n, params.n_q_heads, D), dev), _stream_on(stream, dev)))
 
 
 def draft_attention_workspace_size(ctx: Context, params: tu_attn_params, draft: Draft) -> int:
@@ -669,9 +685,9 @@ def draft_attention(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     qp = _need(q_hat, "q_hat", torch.bfloat16, shape, dev)
     op = _need(out, "out", torch.bfloat16, shape, dev)
     if workspace is None:
-        workspace = _workspace(draft_attention_workspace_size(ctx, params, draft), dev, None, stream)
+        workspace = _workspace(draft_attention_workspace_size(ctx, params, draft), q_hat.device, None, stream)
     _check(lib().draft_attention(ctypes.byref(ctx.c), kc, vc, ctypes.byref(params), draft._ref, qp, op,
-                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+                                 *_workspace_of(workspace, dev), _stream_on(stream, dev)))
     return workspace
 
 
@@ -679,7 +695,7 @@ def draft_short_conv(draft: Draft, items, activation: str = "silu", stream=None)
     """items: sequence of (state [W-1][C], x [n][C], weight [C][W], out [n][C]) bf16 tensors sharing one width: the
     convolution along each node's path, the states only read."""
     arr = (tu_conv_tensor * max(1, len(items)))()
-    W, bf = None, torch.bfloat16
+    W, bf, dev = None, torch.bfloat16, -1
     for i, (st, x, w, out) in enumerate(items):
         dev = _call_device(x)
         C = int(x.shape[1])
@@ -691,7 +707,7 @@ def draft_short_conv(draft: Draft, items, activation: str = "silu", stream=None)
         t.state = None if st is None else _need(st, "state", bf, (W - 1, C), dev)
         t.x, t.weight = _need(x, "x", bf, rows, dev), _need(w, "weight", bf, (C, W), dev)
         t.out, t.T, t.channels = _need(out, "out", bf, rows, dev), draft.n, C
-    _check(lib().draft_short_conv(draft._ref, arr, len(items), W or 1, _ACTIVATIONS[activation], _stream(stream)))
+    _check(lib().draft_short_conv(draft._ref, arr, len(items), W or 1, _ACTIVATIONS[activation], _stream_on(stream, dev)))
 
 
 def draft_delta_rule(state: torch.Tensor, q, k, v, beta, g, params: tu_delta_params, draft: Draft, out: torch.Tensor,
@@ -704,7 +720,7 @@ def draft_delta_rule(state: torch.Tensor, q, k, v, beta, g, params: tu_delta_par
                                   _need(k, "k", bf, (n, Hk, d), dev), _need(v, "v", bf, (n, Hv, d), dev),
                                   _need(beta, "beta", f32, (n, Hv), dev), _need(g, "g", f32, (n, Hv), dev),
                                   ctypes.byref(params), draft._ref, _need(out, "out", f32, (n, Hv, d), dev),
-                                  _stream(stream)))
+                                  _stream_on(stream, dev)))
 
 
 def draft_verify_workspace_size(draft: Draft, vocab: int) -> int:
@@ -719,20 +735,20 @@ def draft_verify(draft: Draft, tokens: torch.Tensor, target: torch.Tensor, unifo
     dev, n, V = _call_device(target), draft.n, int(target.shape[-1])
     f32 = torch.float32
     if result is None:
-        result = torch.empty(n + 2, dtype=torch.int32, device=dev)
-        ts = _torch_stream(stream, dev)
-        if ts is not None and ts != torch.cuda.current_stream(dev):
+        result = torch.empty(n + 2, dtype=torch.int32, device=target.device)
+        ts = _torch_stream(stream, target.device)
+        if ts is not None and ts != torch.cuda.current_stream(target.device):
             result.record_stream(ts)
     if workspace is None:
-        workspace = _workspace(draft_verify_workspace_size(draft, V), dev, None, stream)
-    tp = _need(target, "target", f32, (n, V), dev, 1)
-    pp = None if proposal is None else _need(proposal, "proposal", f32, (n, V), dev, 1)
+        workspace = _workspace(draft_verify_workspace_size(draft, V), target.device, None, stream)
+    tp = _need(target, "target", f32, (n, V), dev, True)
+    pp = None if proposal is None else _need(proposal, "proposal", f32, (n, V), dev, True)
     _check(lib().draft_verify(draft._ref, _need(tokens, "tokens", torch.int32, (n,), dev), tp,
                               target.stride(0) if n > 1 else V, pp,
                               0 if proposal is None else proposal.stride(0) if n > 1 else V, V,
                               _need(uniforms, "uniforms", f32, (n,), dev),
-                              _need(result, "result", torch.int32, (n + 2,), dev), workspace.data_ptr(),
-                              workspace.numel() * workspace.element_size(), _stream(stream)))
+                              _need(result, "result", torch.int32, (n + 2,), dev), *_workspace_of(workspace, dev),
+                              _stream_on(stream, dev)))
     return result
 
 
@@ -749,7 +765,7 @@ class DraftStack:
         tensors = [t for L in layers for t in ((L.k_cache or [None])[0], (L.state or [None])[0]) if t is not None]
         tensors += [st for st, _ in convs]
         if tensors:
-            self.device = tensors[0].device
+            self.device = tensors[0].get_device()
 
         def rows(t, what):
             if self.rows is not None and t.shape[0] != self.rows:
@@ -803,13 +819,14 @@ def draft_accept(ctx: Context, draft: Draft, path: Sequence[int], stack: DraftSt
         raise ValueError(f"the stack's tensors have {stack.rows} rows, the draft {draft.n} nodes")
     if stack.capacity is not None and stack.capacity < ctx.c.capacity:
         raise ValueError(f"a cache has {stack.capacity} rows, the context's capacity is {ctx.capacity}")
-    if _call_device(ctx.pos) != (stack.device or ctx.pos.device):
-        raise ValueError(f"the context is on {ctx.pos.device}, its layers on {stack.device}")
+    dev = _call_device(ctx.pos)
+    if stack.device is not None and stack.device != dev:
+        raise ValueError(f"the context is on device {dev}, its layers on device {stack.device}")
     _check(lib().draft_accept(ctypes.byref(ctx.c), draft._ref, (_i32 * max(1, len(path)))(*path), len(path),
                               stack._layers, stack.n_layers,
                               None if stack.attn is None else ctypes.byref(stack.attn),
                               None if stack.delta is None else ctypes.byref(stack.delta), stack._convs, stack.n_convs,
-                              stack.width, _stream(stream)))
+                              stack.width, _stream_on(stream, dev)))
 
 
 TU_FAULT_POSITIONS = 1   # device positions disagreed with the host's live runs

@@ -91,9 +91,9 @@ void norm_record(const tu_attn_params* p, const tu_qk_norm* norm, int64_t T, Nor
 int draft_splits(const tu_attn_params* p, int64_t n, int64_t len) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   const int64_t tiles = (n * G + kDraftRows - 1) / kDraftRows;
-  const int64_t stages = (len + n + draft_stage_keys(p->head_dim) - 1) / draft_stage_keys(p->head_dim);
+  const int64_t units = (len + n + kDraftUnit - 1) / kDraftUnit;
   const int64_t want = p->kv_splits > 0 ? p->kv_splits : kCus / std::max<int64_t>(1, p->n_kv_heads * tiles);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, stages, 128}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, units, kMaxDraftSplits}));
 }
 
 size_t attention_ws(const tu_attn_params* p, int64_t n, int splits) {

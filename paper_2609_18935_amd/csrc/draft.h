@@ -41,7 +41,7 @@ struct DraftAttnArgs {
   const bf16_t* v_cache;
   bf16_t* out;            // [n][Hq][D]
   _Float16* part_o;       // [splits][n * Hq][D] normalised partial outputs (unused when n_splits == 1)
-  float* part_ml;         // [splits][n * Hq][2] reference max (log2 units), sum
+  float* part_ml;         // [n * Hq][splits][2] reference max (log2 units), sum
   CallStatus status;
   int32_t len;
   int32_t n;
@@ -53,9 +53,9 @@ struct DraftAttnArgs {
   int32_t pad;
   DraftMasks seen;
 };
+constexpr int kMaxDraftSplits = 128;
 constexpr int kDraftRows = 256;         // packed query rows of an attention workgroup
-constexpr int kDraftStageBytes = 16384; // K (or V) bytes of one stage
-constexpr int draft_stage_keys(int D) { return kDraftStageBytes / (2 * D); }
+constexpr int kDraftUnit = 32;          // keys of a unit
 
 struct DraftConvArgs {
   ConvJob job[kMaxConvJobs];   // state is only read

@@ -2,25 +2,28 @@
 // ancestors' rows and its own.
 //
 // The G query heads of a KV head are packed as rows (row = node * G + h mod G). A workgroup
-// takes 256 rows (8 waves of 32) of one KV head and one split of the key range. K and V come
-// as they lie in the cache, in stages of 16 KB each (32 keys of 256 dims), by LDS DMA into a
-// ring of four, three of them in flight: the cache is asked for far ahead whatever the number
+// takes 256 rows (8 waves of 32, two per SIMD) of one KV head and one split of the key range.
+// K and V come as they lie in the cache, in units of 32 keys, by LDS DMA into rings of four
+// units, two to three of them in flight: the cache is asked for far ahead whatever the number
 // of rows, and waves without rows only load.
 //
 // S^T = K Q^T on v_mfma_f32_32x32x16_bf16, so that a lane holds 16 keys of one query and the
 // running maximum and sum are per lane. P is rounded to f16 (10 stored mantissa bits; bf16's 7
 // would add an error as large as the output's own rounding), so V must be f16 too: every
-// thread turns the chunks that it has itself loaded into f16 in place, before the barrier that
-// shows the stage to the others. O^T += V^T P^T on the f16 MFMA, V transposed on its way by
-// ds_read_b64_tr_b16. Softmax sums, the running maximum (moved only when exceeded by 2^8) and
-// O are fp32.
+// thread turns the chunks that it has itself loaded into f16 in place, a barrier before anyone
+// reads them. O^T += V^T P^T on the f16 MFMA, V transposed on its way by ds_read_b64_tr_b16.
+// Softmax sums, the running maximum (moved only when exceeded by 2^8) and O are fp32.
+//
+// The two waves of a SIMD take turns: while waves 0 - 3 run the matrix products of a unit (P V of the
+// unit before, then K Q^T), waves 4 - 7 run the softmax of theirs, and a barrier later the
+// other way round, so that the matrix core always has a wave to feed it.
 //
 // A row of D dims lies in LDS as D / 8 chunks of 16 bytes, permuted within the row so that the
 // rows read together fall into different banks: chunk c of K row r at c ^ (r mod 16), of V row
-// r at c ^ 2 (r mod 8); less where a row has fewer chunks.
+// r at c ^ 2 (r mod 8); less where a row has fewer chunks. Outputs leave through LDS as well, in whole rows.
 //
-// The tree only matters to the units of 32 keys that reach past row len: there each lane
-// shifts its node's mask to the unit and drops the keys whose bit is clear.
+// The tree only matters to the units that reach past row len: there each lane shifts its
+// node's mask to the unit and drops the keys whose bit is clear.
 #include "attention_tile.h"
 #include "draft.h"
 
@@ -29,36 +32,32 @@ namespace tu {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kStages = 4;
-constexpr int kLoads = 4;   // DMA loads of a thread for a stage: two of K, two of V
+constexpr int kUnit = kDraftUnit;
 constexpr int kLgkmWait0 = 15 | (7 << 4) | (0 << 8) | (3 << 14);
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-// One array per stage and tensor, so that the compiler sees that the DMA into one does not
-// alias the reads of another.
-__shared__ __attribute__((aligned(16))) char g_k0[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_k1[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_k2[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_k3[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_v0[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_v1[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_v2[kDraftStageBytes];
-__shared__ __attribute__((aligned(16))) char g_v3[kDraftStageBytes];
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 
 template <int B>
 struct IntC {
   static constexpr int value = B;
 };
-template <int B>
-__device__ __forceinline__ char* stage_k() {
-  return B == 0 ? g_k0 : B == 1 ? g_k1 : B == 2 ? g_k2 : g_k3;
-}
-template <int B>
-__device__ __forceinline__ char* stage_v() {
-  return B == 0 ? g_v0 : B == 1 ? g_v1 : B == 2 ? g_v2 : g_v3;
-}
+
+// One array per unit and tensor, so that the compiler sees that the DMA into one does not
+// alias the reads of another.
+template <int D>
+struct Ring {
+  static constexpr int kBytes = kUnit * D * 2;
+  static __device__ __forceinline__ char* k(int b) {
+    __shared__ __attribute__((aligned(16))) char k0[kBytes], k1[kBytes], k2[kBytes], k3[kBytes];
+    return b == 0 ? k0 : b == 1 ? k1 : b == 2 ? k2 : k3;
+  }
+  static __device__ __forceinline__ char* v(int b) {
+    __shared__ __attribute__((aligned(16))) char v0[kBytes], v1[kBytes], v2[kBytes], v3[kBytes];
+    return b == 0 ? v0 : b == 1 ? v1 : b == 2 ? v2 : v3;
+  }
+};
 
 // Barrier that does not wait for the loads in flight.
 __device__ __forceinline__ void wg_barrier() {
@@ -73,10 +72,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   constexpr int NS = D / 16;                 // 16-dim steps of S^T = K Q^T
   constexpr int NDB = D / 32;                // 32-dim blocks of O^T
   constexpr int RC = D / 8;                  // 16-byte chunks per row
-  constexpr int SK = draft_stage_keys(D);    // keys of a stage
   constexpr int KSWZ = RC < 16 ? RC - 1 : 15;
   constexpr int VSWZ = RC / 2 < 8 ? RC / 2 - 1 : 7;
-  static_assert(SK * RC == 2 * kThreads, "two chunks of K and of V per thread and stage");
+  constexpr int NC = kUnit * RC;             // chunks of a unit of K (or V)
+  constexpr bool kHalf = NC < kThreads;      // waves 0 - 3 load K, waves 4 - 7 load V (each loads both otherwise)
+  constexpr int NL = kHalf ? 1 : NC / kThreads;   // loads of a thread for a unit of K or V
+  constexpr int PER = kHalf ? 1 : 2 * NL;         // loads of a thread for a unit
+  static_assert(kHalf ? NC == kThreads / 2 : NC % kThreads == 0, "whole loads per thread");
+  typedef Ring<D> R;
+  __shared__ uint64_t s_mask[kDraftRows][2];   // masks of the rows' nodes (workgroups that reach the tree)
+  __shared__ int s_row[kDraftRows];            // output rows
 
   const int item = xcd_remap(blockIdx.x, gridDim.x);
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
@@ -89,49 +94,63 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int split = __builtin_amdgcn_readfirstlane(local % a.n_splits);
   const int hkv = __builtin_amdgcn_readfirstlane(local / a.n_splits);
   const int len = a.len, n = a.n;
-  const int rows_total = n * G;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hl = lane >> 5, col = lane & 31;
-  const int r = tile * kDraftRows + wave * 32 + col;
-  const bool row_ok = r < rows_total;
-  const int node = row_ok ? r / G : n - 1;
-  const int qh = hkv * G + (row_ok ? r - (r / G) * G : 0);
   const int n_valid = len + n;
-  const int n_st = (n_valid + SK - 1) / SK;
-  const int st0 = (int)((long)n_st * split / a.n_splits), st1 = (int)((long)n_st * (split + 1) / a.n_splits);
+  const int n_units = (n_valid + kUnit - 1) / kUnit;
+  const int u0 = (int)((long)n_units * split / a.n_splits), u1 = (int)((long)n_units * (split + 1) / a.n_splits);
   const long rs = (long)Hkv * D;
   const bf16_t* kbase = a.k_cache + (long)hkv * D;
   const bf16_t* vbase = a.v_cache + (long)hkv * D;
 
-  bf16x8 qf[NS];
-  {
-    const bf16_t* qrow = a.q_hat + ((long)node * Hq + qh) * D + 8 * hl;   // rows past the last repeat one (dropped)
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + 16 * s));
-  }
-
-  // ---- a stage: LDS chunk i * 512 + tid of K and of V is loaded by load i of the thread.
-  // The resource ends at the cache's data: rows past it, and stages past the split, are zeros.
-  // The second load's row lies a multiple of 16 (of 8 with 8 chunks) rows on: the same chunk.
+  // ---- a unit: LDS chunk i * 512 + tid is loaded by load i of the thread. The resource ends
+  // at the cache's data: rows past it, and units past the split, are zeros.
+  // A further load's row lies a multiple of 16 rows on: the same chunk.
   constexpr int LR = kThreads / RC;
-  static_assert(LR % (KSWZ + 1) == 0 && LR % (VSWZ + 1) == 0, "both loads of a thread take the same chunk");
-  const int lrow = tid / RC, lc = tid % RC;
-  const uint32_t koff = (uint32_t)(lrow * (int)rs * 2 + (lc ^ (lrow & KSWZ)) * 16);
+  static_assert(kHalf || (LR % (KSWZ + 1) == 0 && LR % (VSWZ + 1) == 0), "the loads of a thread take the same chunk");
+  const int ltid = kHalf ? tid & (kThreads / 2 - 1) : tid;
+  const int lwave = kHalf ? wave & 3 : wave;
+  const int lrow = ltid / RC, lc = ltid % RC;
+  const bool lv = kHalf && wave >= 4;
+  const uint32_t koff = (uint32_t)(lrow * (int)rs * 2 + (lc ^ (lv ? 2 * (lrow & VSWZ) : lrow & KSWZ)) * 16);
   const uint32_t voff = (uint32_t)(lrow * (int)rs * 2 + (lc ^ (2 * (lrow & VSWZ))) * 16);
   const uint32_t lstep = (uint32_t)(LR * (int)rs * 2);
-  auto load = [&](auto bc, int st) __attribute__((always_inline)) {
-    constexpr int B = decltype(bc)::value;
-    const int key0 = st * SK;
-    const int bytes = st < st1 ? min(n_valid - key0, SK) * (int)rs * 2 - ((int)rs - D) * 2 : 0;
-    const long off = (long)key0 * rs;
+  auto dma = [&](const bf16_t* head, uint32_t off, char* dst, int u) __attribute__((always_inline)) {
+    const int key0 = u * kUnit;
+    const int bytes = u < u1 ? min(n_valid - key0, kUnit) * (int)rs * 2 - ((int)rs - D) * 2 : 0;
+    const bf16_t* base = head + (long)key0 * rs;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      dma16(kbase + off, bytes, koff, i * lstep, stage_k<B>() + (i * kThreads + wave * 64) * 16);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      dma16(vbase + off, bytes, voff, i * lstep, stage_v<B>() + (i * kThreads + wave * 64) * 16);
+    for (int i = 0; i < NL; ++i) dma16(base, bytes, off, i * lstep, dst + (i * kThreads + lwave * 64) * 16);
   };
+  auto load_k = [&](auto bc, int u) __attribute__((always_inline)) {
+    if (!lv) dma(kbase, koff, R::k(decltype(bc)::value), u);
+  };
+  auto load_v = [&](auto bc, int u) __attribute__((always_inline)) {
+    if (!kHalf) dma(vbase, voff, R::v(decltype(bc)::value), u);
+    else if (lv) dma(vbase, koff, R::v(decltype(bc)::value), u);
+  };
+
+  // the first units are asked for before anything else; then Q (only the first unit is waited
+  // for with it)
+  load_k(IntC<0>{}, u0);
+  const int rows_total = n * G;
+  const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
+  bf16x8 qf[NS];
+  if (busy) {
+    const int r = tile * kDraftRows + wave * 32 + col;
+    const int node = min(r / G, n - 1);
+    const int row = r < rows_total ? node * Hq + hkv * G + (r - node * G) : node * Hq + hkv * G;   // past the last: dropped
+    const bf16_t* qrow = a.q_hat + (long)row * D + 8 * hl;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + 16 * s));
+    if (hl == 0) s_row[wave * 32 + col] = r < rows_total ? row : -1;
+    if (u1 * kUnit > len) s_mask[wave * 32 + col][hl] = a.seen.m[node][hl];
+  }
+  load_v(IntC<0>{}, u0);
+  load_k(IntC<1>{}, u0 + 1);
+  load_v(IntC<1>{}, u0 + 1);
+  load_k(IntC<2>{}, u0 + 2);
 
   f32x16 o[NDB];
 #pragma unroll
@@ -142,27 +161,34 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const float c2 = a.scale_log2;
   bool big = false;
 
-  // transposing reads of V (see the unit below): block db lies 256 bytes behind block db - 4
-  constexpr int NVA = NDB < 4 ? NDB : 4;
-  uint32_t vaddr[NVA];
+  // transposing reads of V (see pv below): block db of 32 dims lies at this address ^ 64 db (256
+  // bytes on for each four blocks)
+  uint32_t vaddr;
   {
     const int i = lane & 15, g = lane >> 4;
     const int row = 4 * (g >> 1) + (i >> 2);
     const int c0 = 2 * (g & 1) + ((i & 3) >> 1);
-#pragma unroll
-    for (int db = 0; db < NVA; ++db)
-      vaddr[db] = (uint32_t)(row * D * 2 + (((4 * db + c0) ^ (2 * (row & VSWZ))) * 16) + (i & 1) * 8);
+    vaddr = (uint32_t)(row * D * 2 + ((c0 ^ (2 * (row & VSWZ))) * 16) + (i & 1) * 8);
   }
-
   // K row `col`, chunk hl ^ (col mod 16); chunk 2 s + hl is this address ^ 32 s
   const uint32_t kaddr = (uint32_t)(col * D * 2 + ((hl ^ (col & KSWZ)) * 16));
 
-  // ---- this thread's two chunks of V to f16, in place
+  // (what is derived from these is formed per unit: hoisted, it would cost registers)
+  auto fresh = [](uint32_t x) __attribute__((always_inline)) -> uint32_t {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+
+  // ---- this thread's loads up to V of unit u and K of the next have landed (two units of
+  // loads are newer); its chunks of V to f16, in place
   auto to_f16 = [&](auto bc) __attribute__((always_inline)) {
     constexpr int B = decltype(bc)::value;
+    __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));
+    asm volatile("" ::: "memory");
+    if (kHalf && !lv) return;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      u32x4* at = (u32x4*)(stage_v<B>() + (i * kThreads + tid) * 16);
+    for (int i = 0; i < NL; ++i) {
+      u32x4* at = (u32x4*)(R::v(B) + (i * kThreads + (kHalf ? fresh(tid) & (kThreads / 2 - 1) : fresh(tid))) * 16);
       const u32x4 w = *at;
       f16x8 x;
 #pragma unroll
@@ -176,27 +202,43 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
   };
 
-  // Keeps n MFMAs fed by their LDS fragment reads (PER reads each), two fragments ahead: bounds the
+  f32x16 sacc;
+  f16x8 pf[2];
+
+  // ---- the matrix products: O^T += V^T P^T of the unit in ring place BV, then S^T of the one in
+  // BK (in this order P is gone when the scores come). LDS reads two fragments ahead: bounds the
   // fragment registers in flight (the compiler would otherwise issue every read up front).
   constexpr int kMfma = 0x008, kDsRead = 0x100;
   auto sched_reads = [&](auto nc, auto per) __attribute__((always_inline)) {
-    constexpr int N = decltype(nc)::value, PER = decltype(per)::value;
-    __builtin_amdgcn_sched_group_barrier(kDsRead, PER, 0);
+    constexpr int N = decltype(nc)::value, READS = decltype(per)::value;
+    __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (i < N - 1) __builtin_amdgcn_sched_group_barrier(kDsRead, PER, 0);
+      if (i < N - 1) __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
       __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
     }
   };
-
-  // ---- 32 keys (unit u of the stage in B, first key kb0)
-  auto unit = [&](auto bc, int u, int kb0) __attribute__((always_inline)) {
+  auto pv = [&](const char* vs) __attribute__((always_inline)) {
+    const uint32_t vx = fresh(vaddr);
+#pragma unroll
+    for (int k16 = 0; k16 < 2; ++k16) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        // lane group g reads keys 4 (g >> 1) + 0 .. 3 (+ 16 k16, + 8) at dims 32 db + 16 (g & 1) ..
+        const char* at = vs + (vx ^ (64 * (db & 3))) + (db >> 2) * 256 + 16 * k16 * D * 2;
+        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * D * 2));
+        const u32x2 w0 = __builtin_bit_cast(u32x2, x0), w1 = __builtin_bit_cast(u32x2, x1);
+        const f16x8 va = __builtin_bit_cast(f16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pf[k16], o[db], 0, 0, 0);
+      }
+    }
+    sched_reads(IntC<2 * NDB>{}, IntC<2>{});
+  };
+  auto qk = [&](auto bc) __attribute__((always_inline)) {
     constexpr int B = decltype(bc)::value;
-    const char* ks = stage_k<B>() + u * 32 * D * 2;
-    uint32_t kx = kaddr;
-    asm volatile("" : "+v"(kx));   // formed per unit: hoisted, the 8 addresses would cost registers
-    const char* vs = stage_v<B>() + u * 32 * D * 2;
-    f32x16 sacc;
+    const char* ks = R::k(B);
+    const uint32_t kx = fresh(kaddr);
 #pragma unroll
     for (int e = 0; e < 16; ++e) sacc[e] = 0.f;
 #pragma unroll
@@ -205,19 +247,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[s], sacc, 0, 0, 0);
     }
     sched_reads(IntC<NS>{}, IntC<1>{});
-    if (kb0 + 31 >= len) {   // reaches the tree (uniform)
-      // bit x of `keys`: this query sees key kb0 + x
+  };
+
+  // ---- softmax of unit u: the mask, the maximum, P in f16 in the key order of the operand
+  auto softmax = [&](int u) __attribute__((always_inline)) {
+    const int d = u * kUnit - len;
+    if (d + kUnit - 1 >= 0) {   // reaches the tree (uniform)
+      // bit x of `keys`: this query sees key u * 32 + x
       uint32_t keys;
-      const int d = kb0 - len;
-      const uint64_t m0 = a.seen.m[node][0], m1 = a.seen.m[node][1];
-      if (d <= 0) {
-        keys = d > -32 ? (uint32_t)(m0 << -d) | ((1u << -d) - 1u) : 0xFFFFFFFFu;
-      } else if (d < 64) {
-        keys = (uint32_t)(m0 >> d | m1 << (64 - d));
-      } else {
-        keys = d < 128 ? (uint32_t)(m1 >> (d - 64)) : 0u;
-      }
-      keys >>= 4 * hl;
+      const uint32_t t = fresh(tid), mr = (t & ~63u) / 2 + (t & 31u);
+      const uint64_t m0 = s_mask[mr][0], m1 = s_mask[mr][1];
+      if (d <= 0) keys = (uint32_t)(m0 << -d) | ((1u << -d) - 1u);
+      else if (d < 64) keys = (uint32_t)(m0 >> d | m1 << (64 - d));
+      else keys = d < 128 ? (uint32_t)(m1 >> (d - 64)) : 0u;
+      keys >>= (t & 32u) >> 3;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (!(keys >> (8 * (e >> 2) + (e & 3)) & 1)) sacc[e] = -__builtin_inff();
@@ -237,7 +280,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int db = 0; db < NDB; ++db) scale_acc(o[db], alpha);
     }
     const float m_use = m_run == -__builtin_inff() ? 0.f : m_run;
-    f16x8 pf[2];
     float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -246,119 +288,135 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       pf[e >> 3][e & 7] = (_Float16)p;
     }
     l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
-    // lane group g reads keys 4 (g >> 1) + 0 .. 3 (+ 16 ks, + 8) at dims 32 db + 16 (g & 1) ..
-#pragma unroll
-    for (int k16 = 0; k16 < 2; ++k16) {
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) {
-        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + vaddr[db & 3] + (db >> 2) * 256 + (16 * k16) * D * 2));
-        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + vaddr[db & 3] + (db >> 2) * 256 + (16 * k16 + 8) * D * 2));
-        const u32x2 w0 = __builtin_bit_cast(u32x2, x0), w1 = __builtin_bit_cast(u32x2, x1);
-        const f16x8 va = __builtin_bit_cast(f16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pf[k16], o[db], 0, 0, 0);
-      }
-    }
-    sched_reads(IntC<2 * NDB>{}, IntC<2>{});
   };
 
-  const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
-  auto step = [&](auto bc, int st) __attribute__((always_inline)) {
+  // Unit u in ring place B. K of unit u - 1 and V of unit u - 2 are no longer read after the
+  // first barrier: their places take units u + 3 and u + 2.
+  auto refill = [&](auto bc, int u) __attribute__((always_inline)) {
     constexpr int B = decltype(bc)::value;
-    __builtin_amdgcn_s_waitcnt(vm_wait((kStages - 2) * kLoads));   // this thread's loads of the stage have landed
-    asm volatile("" ::: "memory");
-    to_f16(bc);
-    wg_barrier();   // everyone's have; everyone is done with the stage before
-    load(IntC<(B + kStages - 1) % kStages>{}, st + kStages - 1);
+    load_k(IntC<(B + 3) & 3>{}, u + 3);
+    load_v(IntC<(B + 2) & 3>{}, u + 2);
+  };
+  auto early = [&](auto bc, int u) __attribute__((always_inline)) {   // waves 0 - 3
+    constexpr int B = decltype(bc)::value;
+    wg_barrier();
+    refill(bc, u);
     if (busy) {
-#pragma unroll
-      for (int u = 0; u < SK / 32; ++u) {
-        const int kb0 = st * SK + 32 * u;
-        if (SK == 32 || kb0 < n_valid) unit(bc, u, kb0);
-      }
+      if (u > u0) pv(R::v((B + 3) & 3));
+      qk(bc);
+    }
+    wg_barrier();
+    if (busy) softmax(u);
+    to_f16(bc);
+  };
+  auto late = [&](auto bc, int u) __attribute__((always_inline)) {    // waves 4 - 7
+    constexpr int B = decltype(bc)::value;
+    wg_barrier();
+    refill(bc, u);
+    if (busy && u > u0) softmax(u - 1);
+    to_f16(bc);
+    wg_barrier();
+    if (busy) {
+      if (u > u0) pv(R::v((B + 3) & 3));
+      qk(bc);
     }
   };
-
-  if (st0 < st1) {
-    load(IntC<0>{}, st0);
-    load(IntC<1>{}, st0 + 1);
-    load(IntC<2>{}, st0 + 2);
-    for (int st = st0; st < st1; st += kStages) {
-      step(IntC<0>{}, st);
-      if (st + 1 < st1) step(IntC<1>{}, st + 1);
-      if (st + 2 < st1) step(IntC<2>{}, st + 2);
-      if (st + 3 < st1) step(IntC<3>{}, st + 3);
+  auto run = [&](auto step) __attribute__((always_inline)) {
+    for (int u = u0; u < u1; u += 4) {
+      step(IntC<0>{}, u);
+      if (u + 1 < u1) step(IntC<1>{}, u + 1);
+      if (u + 2 < u1) step(IntC<2>{}, u + 2);
+      if (u + 3 < u1) step(IntC<3>{}, u + 3);
     }
-    __builtin_amdgcn_s_waitcnt(vm_wait(0));   // no load may outlive the workgroup
+  };
+  __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));   // K of the first unit
+  if (wave < 4) run(early);
+  else run(late);
+  __builtin_amdgcn_s_waitcnt(vm_wait(0));   // the loads past the split's end: no write into LDS may come later
+  wg_barrier();
+  if (busy) {
+    if (wave >= 4) softmax(u1 - 1);
+    pv(R::v((u1 - 1 - u0) & 3));   // no load is in flight: the place may be any
   }
   if (big) status_raise(a.status, kFaultRange);
+  wg_barrier();   // the rings are written over below
+  if (!busy) return;
+  const uint32_t te = fresh(tid);
+  const int lane_e = te & 63, col_e = te & 31, hl_e = (te >> 5) & 1;
 
   const auto lsw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, l_run),
                                                     __builtin_bit_cast(uint32_t, l_run), false, false);
   const float l_tot = __builtin_bit_cast(float, (uint32_t)lsw[0]) + __builtin_bit_cast(float, (uint32_t)lsw[1]);
-  if (!row_ok) return;
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;   // 0: no key of this split is seen; NaN goes on
-  const long row = (long)node * Hq + qh;
-  if (a.n_splits == 1) {
-    bf16_t* orow = a.out + row * D;
+  const bool whole = a.n_splits == 1;
+  const int row = s_row[wave * 32 + col_e];
+  if (!whole && hl_e == 0 && row >= 0) {
+    float* ml = a.part_ml + ((long)row * a.n_splits + split) * 2;
+    ml[0] = l_tot == 0.f ? -__builtin_inff() : m_run == -__builtin_inff() ? 0.f : m_run;
+    ml[1] = l_tot;
+  }
+  // the wave's 32 rows through its own place of the rings, then 16 bytes a lane in whole rows
+  char* const mine = wave < 4 ? R::k(wave) : R::v(wave - 4);
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+  for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
-        const bf16x4 v = {(__bf16)(o[db][4 * i] * inv), (__bf16)(o[db][4 * i + 1] * inv),
-                          (__bf16)(o[db][4 * i + 2] * inv), (__bf16)(o[db][4 * i + 3] * inv)};
-        *(bf16x4*)(orow + db * 32 + 8 * i + 4 * hl) = v;
-      }
-  } else {
-    const long prow = (long)split * n * Hq + row;
-    _Float16* orow = a.part_o + prow * D;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f16x4 v = {(_Float16)(o[db][4 * i] * inv), (_Float16)(o[db][4 * i + 1] * inv),
-                         (_Float16)(o[db][4 * i + 2] * inv), (_Float16)(o[db][4 * i + 3] * inv)};
-        *(f16x4*)(orow + db * 32 + 8 * i + 4 * hl) = v;
-      }
-    if (hl == 0) {
-      a.part_ml[prow * 2] = l_tot == 0.f ? -__builtin_inff() : m_run == -__builtin_inff() ? 0.f : m_run;
-      a.part_ml[prow * 2 + 1] = l_tot;
+    for (int i = 0; i < 4; ++i) {
+      char* at = mine + col_e * D * 2 + (((4 * db + i) ^ (col_e & KSWZ)) * 16) + hl_e * 8;
+      const float x0 = o[db][4 * i] * inv, x1 = o[db][4 * i + 1] * inv, x2 = o[db][4 * i + 2] * inv, x3 = o[db][4 * i + 3] * inv;
+      if (whole) *(bf16x4*)at = bf16x4{(__bf16)x0, (__bf16)x1, (__bf16)x2, (__bf16)x3};
+      else *(f16x4*)at = f16x4{(_Float16)x0, (_Float16)x1, (_Float16)x2, (_Float16)x3};
     }
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(kLgkmWait0);
+  char* const to = whole ? (char*)a.out : (char*)(a.part_o + (long)split * n * Hq * D);
+#pragma unroll
+  for (int i = 0; i < kUnit * RC / 64; ++i) {
+    const int q = i * 64 + lane_e, rr = q / RC, c = q % RC;
+    const u32x4 x = *(const u32x4*)(mine + rr * D * 2 + ((c ^ (rr & KSWZ)) * 16));
+    const int orow = s_row[wave * 32 + rr];
+    if (orow >= 0) *(u32x4*)(to + ((long)orow * D + 8 * c) * 2) = x;
   }
 }
 
-// Joins the splits of one (node, head) row a workgroup: D / 4 lanes hold the row, 4 dims each,
-// the lane groups take the splits in turn and are added up through LDS in a fixed order.
+// Joins the splits: a workgroup takes 64 dims of one (node, head) row, 16 lanes of 4 dims; its
+// 16 lane groups take the splits in turn and are added up through LDS in a fixed order. Every
+// lane requests all of its splits at once, before the weights are known: one trip to memory.
 constexpr int kMergeThreads = 256;
+constexpr int kMergeDims = 64;
+constexpr int kMergeLanes = kMergeDims / 4;
+constexpr int kMergeGroups = kMergeThreads / kMergeLanes;
+constexpr int kMergeEach = kMaxDraftSplits / kMergeGroups;   // splits of a lane group
+static_assert(kMaxDraftSplits == 128, "two splits per lane of a wave");
+
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) {
-  constexpr int LANES = D / 4;
-  constexpr int GROUPS = kMergeThreads / LANES;
-  __shared__ float s_w[128];
-  __shared__ __attribute__((aligned(16))) float s_o[GROUPS][D];
-  const long row = blockIdx.x, R = (long)a.n * a.n_q_heads;
-  const int tid = threadIdx.x, g = tid / LANES, l = tid % LANES;
-  // weights of the splits: every wave forms them alike
-  const int lane = tid & 63;
-  float m[2], w[2];
+  __shared__ float s_w[kMaxDraftSplits];
+  __shared__ __attribute__((aligned(16))) float s_o[kMergeGroups][kMergeDims];
+  constexpr int SLICES = D / kMergeDims;
+  const int row = blockIdx.x / SLICES, d0 = (blockIdx.x % SLICES) * kMergeDims;
+  const long R = (long)a.n * a.n_q_heads;
+  const int tid = threadIdx.x, lane = tid & 63, g = tid / kMergeLanes, l = tid % kMergeLanes;
+  const int ns = a.n_splits;
+  const float* ml = a.part_ml + (long)row * ns * 2;
+  typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+  f32x2 x[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int s = lane + 64 * i;
-    m[i] = -__builtin_inff();
-    w[i] = 0.f;
-    if (s < a.n_splits) {
-      const float* ml = a.part_ml + ((long)s * R + row) * 2;
-      m[i] = ml[0];
-      w[i] = ml[1];
-    }
+  for (int i = 0; i < 2; ++i) x[i] = lane + 64 * i < ns ? *(const f32x2*)(ml + 2 * (lane + 64 * i)) : f32x2{-__builtin_inff(), 0.f};
+  const _Float16* po = a.part_o + (long)row * D + d0 + 4 * l;
+  f16x4 v[kMergeEach];
+#pragma unroll
+  for (int i = 0; i < kMergeEach; ++i) {
+    const int s = g + kMergeGroups * i;
+    v[i] = s < ns ? *(const f16x4*)(po + (long)s * R * D) : f16x4{};
   }
-  float M = fmaxf(m[0], m[1]);
+  // weights of the splits: every wave forms them alike, the first one stores them
+  float M = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
-  float L = 0.f;
+  float w[2], L = 0.f;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    w[i] = m[i] == -__builtin_inff() ? 0.f : w[i] * __builtin_amdgcn_exp2f(m[i] - M);
+    w[i] = x[i][0] == -__builtin_inff() ? 0.f : x[i][1] * __builtin_amdgcn_exp2f(x[i][0] - M);
     L += w[i];
   }
 #pragma unroll
@@ -369,23 +427,19 @@ __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) 
   }
   __syncthreads();
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  const _Float16* po = a.part_o + row * D + 4 * l;
-#pragma unroll 8
-  for (int s = g; s < a.n_splits; s += GROUPS) {
-    const float ws = s_w[s];
-    const f16x4 v = *(const f16x4*)(po + (long)s * R * D);
-    if (ws != 0.f) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += ws * (float)v[e];
-    }
+  for (int i = 0; i < kMergeEach; ++i) {
+    const float ws = s_w[g + kMergeGroups * i];   // 0 past the last split
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(ws, (float)v[i][e], acc[e]);
   }
   *(f32x4*)&s_o[g][4 * l] = acc;
   __syncthreads();
-  for (int d = tid; d < D; d += kMergeThreads) {
+  if (tid < kMergeDims) {
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) sum += s_o[i][d];
-    ((__bf16*)a.out)[row * D + d] = (__bf16)(sum / L);
+    for (int i = 0; i < kMergeGroups; ++i) sum += s_o[i][tid];
+    ((__bf16*)a.out)[(long)row * D + d0 + tid] = (__bf16)(sum / L);
   }
 }
 
@@ -408,9 +462,9 @@ hipError_t launch_draft_merge(const DraftAttnArgs& a, int head_dim, hipStream_t 
   const int rows = a.n * a.n_q_heads;
   if (rows <= 0) return hipSuccess;
   switch (head_dim) {
-    case 256: hipLaunchKernelGGL(k_draft_merge<256>, dim3(rows), dim3(kMergeThreads), 0, s, a); break;
-    case 128: hipLaunchKernelGGL(k_draft_merge<128>, dim3(rows), dim3(kMergeThreads), 0, s, a); break;
-    case 64: hipLaunchKernelGGL(k_draft_merge<64>, dim3(rows), dim3(kMergeThreads), 0, s, a); break;
+    case 256: hipLaunchKernelGGL(k_draft_merge<256>, dim3(rows * 4), dim3(kMergeThreads), 0, s, a); break;
+    case 128: hipLaunchKernelGGL(k_draft_merge<128>, dim3(rows * 2), dim3(kMergeThreads), 0, s, a); break;
+    case 64: hipLaunchKernelGGL(k_draft_merge<64>, dim3(rows * 1), dim3(kMergeThreads), 0, s, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
