@@ -92,7 +92,11 @@ int draft_splits(const tu_attn_params* p, int64_t n, int64_t len) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   const int64_t tiles = (n * G + kDraftRows - 1) / kDraftRows;
   const int64_t units = (len + n + kDraftUnit - 1) / kDraftUnit;
-  const int64_t want = p->kv_splits > 0 ? p->kv_splits : kCus / std::max<int64_t>(1, p->n_kv_heads * tiles);
+  int64_t want = p->kv_splits > 0 ? p->kv_splits : kCus / std::max<int64_t>(1, p->n_kv_heads * tiles);
+  // a split's rows span less than 2^31 bytes (its loads' offsets are 32 bits wide), with the
+  // units loaded past its end
+  const int64_t unit_bytes = (int64_t)kDraftUnit * p->n_kv_heads * p->head_dim * 2;
+  want = std::max(want, (units * unit_bytes) / (INT32_MAX - 8 * unit_bytes) + 1);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, units, kMaxDraftSplits}));
 }
 
@@ -248,8 +252,17 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     a.n = n;
     a.n_q_heads = p->n_q_heads;
     a.n_kv_heads = p->n_kv_heads;
-    a.n_tiles = (n * (p->n_q_heads / p->n_kv_heads) + kDraftRows - 1) / kDraftRows;
+    a.group = p->n_q_heads / p->n_kv_heads;
+    a.n_tiles = (n * a.group + kDraftRows - 1) / kDraftRows;
     a.n_splits = splits;
+    const int units = (int)((seq->len + n + kDraftUnit - 1) / kDraftUnit);
+    a.split_units = units / splits;
+    a.more_units = units % splits;
+    a.inv_tiles = 1.f / a.n_tiles;
+    a.inv_splits = 1.f / splits;
+    a.inv_group = 1.f / a.group;
+    if ((int64_t)p->n_kv_heads * splits * a.n_tiles >= 1 << 21 || n * a.group >= 1 << 21)
+      return fail(TU_ERR_ARG, "too many heads");
     a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
     draft_masks(draft, &a.seen);
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -49,6 +49,12 @@ struct DraftAttnArgs {
   int32_t n_kv_heads;
   int32_t n_tiles;        // ceil(n * G / kDraftRows)
   int32_t n_splits;
+  int32_t group;          // query heads per KV head
+  int32_t split_units;    // units of 32 keys of a split; the first more_units splits have one more
+  int32_t more_units;
+  float inv_tiles;        // reciprocals
+  float inv_splits;
+  float inv_group;
   float scale_log2;       // softmax_scale * log2(e)
   int32_t pad;
   DraftMasks seen;

@@ -59,6 +59,9 @@ struct Ring {
   }
 };
 
+// x / d for 0 <= x < 2^21, inv = 1 / d: the half keeps the product off every border
+__device__ __forceinline__ int quotient(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
+
 // Barrier that does not wait for the loads in flight.
 __device__ __forceinline__ void wg_barrier() {
   asm volatile("" ::: "memory");
@@ -84,73 +87,108 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ int s_row[kDraftRows];            // output rows
 
   const int item = xcd_remap(blockIdx.x, gridDim.x);
-  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, G = Hq / Hkv;
+  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads;
   if (item >= Hkv * a.n_splits * a.n_tiles) return;
   status_mark(a.status);
   // the row tiles of one key range are neighbours: they share a die's L2
-  int local = item;
-  const int tile = __builtin_amdgcn_readfirstlane(local % a.n_tiles);
-  local /= a.n_tiles;
-  const int split = __builtin_amdgcn_readfirstlane(local % a.n_splits);
-  const int hkv = __builtin_amdgcn_readfirstlane(local / a.n_splits);
-  const int len = a.len, n = a.n;
+  const int range = __builtin_amdgcn_readfirstlane(quotient(item, a.inv_tiles));
+  const int tile = __builtin_amdgcn_readfirstlane(item - range * a.n_tiles);
+  const int hkv = __builtin_amdgcn_readfirstlane(quotient(range, a.inv_splits));
+  const int split = __builtin_amdgcn_readfirstlane(range - hkv * a.n_splits);
+  const int len = a.len, n = a.n, G = a.group;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hl = lane >> 5, col = lane & 31;
-  const int n_valid = len + n;
-  const int n_units = (n_valid + kUnit - 1) / kUnit;
-  const int u0 = (int)((long)n_units * split / a.n_splits), u1 = (int)((long)n_units * (split + 1) / a.n_splits);
-  const long rs = (long)Hkv * D;
-  const bf16_t* kbase = a.k_cache + (long)hkv * D;
-  const bf16_t* vbase = a.v_cache + (long)hkv * D;
+  // units u0 .. u1 - 1: equal shares, the first `more_units` splits one more
+  const int u0 = split * a.split_units + min(split, a.more_units);
+  const int u1 = u0 + a.split_units + (split < a.more_units ? 1 : 0);
+  const int rs = Hkv * D;   // elements of a cache row
 
-  // ---- a unit: LDS chunk i * 512 + tid is loaded by load i of the thread. The resource ends
-  // at the cache's data: rows past it, and units past the split, are zeros.
-  // A further load's row lies a multiple of 16 rows on: the same chunk.
+  // ---- a unit: LDS chunk i * 512 + tid is loaded by load i of the thread. The resources start
+  // at the split's first row and end with its last one that holds data: rows past it, and units
+  // past the split, are zeros. (A split's rows span less than 2^31 bytes.) A further load's
+  // row lies a multiple of 16 rows on: the same chunk.
   constexpr int LR = kThreads / RC;
   static_assert(kHalf || (LR % (KSWZ + 1) == 0 && LR % (VSWZ + 1) == 0), "the loads of a thread take the same chunk");
-  const int ltid = kHalf ? tid & (kThreads / 2 - 1) : tid;
   const int lwave = kHalf ? wave & 3 : wave;
-  const int lrow = ltid / RC, lc = ltid % RC;
   const bool lv = kHalf && wave >= 4;
-  const uint32_t koff = (uint32_t)(lrow * (int)rs * 2 + (lc ^ (lv ? 2 * (lrow & VSWZ) : lrow & KSWZ)) * 16);
-  const uint32_t voff = (uint32_t)(lrow * (int)rs * 2 + (lc ^ (2 * (lrow & VSWZ))) * 16);
-  const uint32_t lstep = (uint32_t)(LR * (int)rs * 2);
-  auto dma = [&](const bf16_t* head, uint32_t off, char* dst, int u) __attribute__((always_inline)) {
-    const int key0 = u * kUnit;
-    const int bytes = u < u1 ? min(n_valid - key0, kUnit) * (int)rs * 2 - ((int)rs - D) * 2 : 0;
-    const bf16_t* base = head + (long)key0 * rs;
+  const long start = (long)u0 * kUnit * rs + (long)hkv * D;
+  const uint32_t bytes = (uint32_t)(min((u1 - u0) * kUnit, len + n - u0 * kUnit) * rs * 2 - (rs - D) * 2);
+  const __amdgpu_buffer_rsrc_t kres =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_cache + start), 0, bytes, kBufWord3);
+  const __amdgpu_buffer_rsrc_t vres =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_cache + start), 0, bytes, kBufWord3);
+  uint32_t koff, voff;   // of the next unit to load
+  {
+    const int ltid = kHalf ? tid & (kThreads / 2 - 1) : tid;
+    const int lrow = ltid / RC, lc = ltid % RC;
+    koff = (uint32_t)(lrow * rs * 2 + (lc ^ (lrow & KSWZ)) * 16);
+    voff = (uint32_t)(lrow * rs * 2 + (lc ^ (2 * (lrow & VSWZ))) * 16);
+  }
+  const uint32_t unit_bytes = (uint32_t)(kUnit * rs * 2);
+  auto dma = [&](const __amdgpu_buffer_rsrc_t res, uint32_t& off, char* dst) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) dma16(base, bytes, off, i * lstep, dst + (i * kThreads + lwave * 64) * 16);
+    for (int i = 0; i < NL; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void*)(dst + (i * kThreads + lwave * 64) * 16), 16, off,
+                                               i * LR * rs * 2, 0, 0);
+    off += unit_bytes;
   };
-  auto load_k = [&](auto bc, int u) __attribute__((always_inline)) {
-    if (!lv) dma(kbase, koff, R::k(decltype(bc)::value), u);
+  auto load_k = [&](auto bc) __attribute__((always_inline)) {
+    if (!lv) dma(kres, koff, R::k(decltype(bc)::value));
   };
-  auto load_v = [&](auto bc, int u) __attribute__((always_inline)) {
-    if (!kHalf) dma(vbase, voff, R::v(decltype(bc)::value), u);
-    else if (lv) dma(vbase, koff, R::v(decltype(bc)::value), u);
+  auto load_v = [&](auto bc) __attribute__((always_inline)) {
+    if (!kHalf || lv) dma(vres, voff, R::v(decltype(bc)::value));
   };
 
-  // the first units are asked for before anything else; then Q (only the first unit is waited
-  // for with it)
-  load_k(IntC<0>{}, u0);
+  // the first units are asked for before anything else; Q is waited for with the first of them
+  load_k(IntC<0>{});
   const int rows_total = n * G;
   const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
+  // Q's rows are read a line at a time (four parts of a row, 64 / LPR rows a load) and go
+  // through the wave's own LDS, in a ring place that is free until the first unit, into the
+  // operands: lane (query, half) holds 8 dims of each 16.
+  constexpr int LPR = D / 32;          // 16-byte chunks of a quarter row
+  constexpr int QL = LPR / 2;          // loads of a quarter
   bf16x8 qf[NS];
+  u32x4 w[NS];
+  uint64_t mask = 0;
   if (busy) {
     const int r = tile * kDraftRows + wave * 32 + col;
-    const int node = min(r / G, n - 1);
-    const int row = r < rows_total ? node * Hq + hkv * G + (r - node * G) : node * Hq + hkv * G;   // past the last: dropped
-    const bf16_t* qrow = a.q_hat + (long)row * D + 8 * hl;
+    const int node = min(quotient(r, a.inv_group), n - 1);
+    const int row = r < rows_total ? node * Hq + hkv * G + (r - node * G) : -1;
+    if (hl == 0) s_row[wave * 32 + col] = row;
+    const bf16_t* from[QL];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + 16 * s));
-    if (hl == 0) s_row[wave * 32 + col] = r < rows_total ? row : -1;
-    if (u1 * kUnit > len) s_mask[wave * 32 + col][hl] = a.seen.m[node][hl];
+    for (int i = 0; i < QL; ++i)
+      from[i] = a.q_hat + (long)max(s_row[wave * 32 + lane / LPR + i * (64 / LPR)], 0) * D + (lane % LPR) * 8;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int i = 0; i < QL; ++i) w[b * QL + i] = *(const u32x4*)(from[i] + b * (D / 4));
+    if (u1 * kUnit > len) mask = a.seen.m[node][hl];
   }
-  load_v(IntC<0>{}, u0);
-  load_k(IntC<1>{}, u0 + 1);
-  load_v(IntC<1>{}, u0 + 1);
-  load_k(IntC<2>{}, u0 + 2);
+  load_v(IntC<0>{});
+  load_k(IntC<1>{});
+  load_v(IntC<1>{});
+  load_k(IntC<2>{});
+  if (busy) {
+    if (u1 * kUnit > len) s_mask[wave * 32 + col][hl] = mask;
+    char* const mine = wave < 4 ? R::k(3) + wave * (8 * D) * 2 : R::v(3) + (wave - 4) * (8 * D) * 2;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < QL; ++i) {
+        const int rr = lane / LPR + i * (64 / LPR);
+        *(u32x4*)(mine + (rr * LPR + ((lane % LPR) ^ (rr & (LPR - 1)))) * 16) = w[b * QL + i];
+      }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < QL; ++i)
+        qf[b * QL + i] = __builtin_bit_cast(
+            bf16x8, *(const u32x4*)(mine + (col * LPR + ((2 * i + hl) ^ (col & (LPR - 1)))) * 16));
+    }
+  }
 
   f32x16 o[NDB];
 #pragma unroll
@@ -188,7 +226,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (kHalf && !lv) return;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      u32x4* at = (u32x4*)(R::v(B) + (i * kThreads + (kHalf ? fresh(tid) & (kThreads / 2 - 1) : fresh(tid))) * 16);
+      u32x4* at = (u32x4*)(R::v(B) + (i * kThreads + (fresh(tid) & (kHalf ? kThreads / 2 - 1 : kThreads - 1))) * 16);
       const u32x4 w = *at;
       f16x8 x;
 #pragma unroll
@@ -206,15 +244,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   f16x8 pf[2];
 
   // ---- the matrix products: O^T += V^T P^T of the unit in ring place BV, then S^T of the one in
-  // BK (in this order P is gone when the scores come). LDS reads two fragments ahead: bounds the
-  // fragment registers in flight (the compiler would otherwise issue every read up front).
-  constexpr int kMfma = 0x008, kDsRead = 0x100;
+  // BK (in this order P is gone when the scores come). LDS reads run kAhead fragments ahead: an
+  // MFMA takes 32 cycles, a read over 100; more would not fit the registers.
+  constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = 3;
   auto sched_reads = [&](auto nc, auto per) __attribute__((always_inline)) {
     constexpr int N = decltype(nc)::value, READS = decltype(per)::value;
-    __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
+    constexpr int AHEAD = kAhead < N ? kAhead : N;
+    __builtin_amdgcn_sched_group_barrier(kDsRead, READS * AHEAD, 0);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (i < N - 1) __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
+      if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
       __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
     }
   };
@@ -292,15 +331,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   // Unit u in ring place B. K of unit u - 1 and V of unit u - 2 are no longer read after the
   // first barrier: their places take units u + 3 and u + 2.
-  auto refill = [&](auto bc, int u) __attribute__((always_inline)) {
+  auto refill = [&](auto bc) __attribute__((always_inline)) {
     constexpr int B = decltype(bc)::value;
-    load_k(IntC<(B + 3) & 3>{}, u + 3);
-    load_v(IntC<(B + 2) & 3>{}, u + 2);
+    load_k(IntC<(B + 3) & 3>{});
+    load_v(IntC<(B + 2) & 3>{});
   };
   auto early = [&](auto bc, int u) __attribute__((always_inline)) {   // waves 0 - 3
     constexpr int B = decltype(bc)::value;
     wg_barrier();
-    refill(bc, u);
+    refill(bc);
     if (busy) {
       if (u > u0) pv(R::v((B + 3) & 3));
       qk(bc);
@@ -312,7 +351,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   auto late = [&](auto bc, int u) __attribute__((always_inline)) {    // waves 4 - 7
     constexpr int B = decltype(bc)::value;
     wg_barrier();
-    refill(bc, u);
+    refill(bc);
     if (busy && u > u0) softmax(u - 1);
     to_f16(bc);
     wg_barrier();
