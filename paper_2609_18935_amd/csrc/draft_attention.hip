@@ -37,6 +37,7 @@ constexpr int kLgkmWait0 = 15 | (7 << 4) | (0 << 8) | (3 << 14);
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 
 template <int B>
@@ -44,20 +45,24 @@ struct IntC {
   static constexpr int value = B;
 };
 
-// One array per unit and tensor, so that the compiler sees that the DMA into one does not
-// alias the reads of another.
-template <int D>
-struct Ring {
-  static constexpr int kBytes = kUnit * D * 2;
-  static __device__ __forceinline__ char* k(int b) {
-    __shared__ __attribute__((aligned(16))) char k0[kBytes], k1[kBytes], k2[kBytes], k3[kBytes];
-    return b == 0 ? k0 : b == 1 ? k1 : b == 2 ? k2 : k3;
-  }
-  static __device__ __forceinline__ char* v(int b) {
-    __shared__ __attribute__((aligned(16))) char v0[kBytes], v1[kBytes], v2[kBytes], v3[kBytes];
-    return b == 0 ? v0 : b == 1 ? v1 : b == 2 ? v2 : v3;
-  }
-};
+// 16 bytes per lane from the buffer at voff + soff to LDS at lds + 16 lane. Written out, so that
+// one loop body can serve every place of the rings: for the compiler's own load it would wait
+// for all loads in flight before any LDS read whose address it cannot tell apart. It has no
+// output register; the kernel waits for it by count, and for all of them before it ends.
+__device__ __forceinline__ void dma_lds(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(lds), "v"(voff), "s"(res), "s"(soff)
+               : "memory", "m0");
+}
+
+// Raw buffer resource of `bytes` bytes: reads past them give zeros.
+__device__ __forceinline__ u32x4 buffer_of(const void* base, uint32_t bytes) {
+  const uint64_t b = (uint64_t)base;
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b),
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)),
+               (uint32_t)__builtin_amdgcn_readfirstlane(bytes), (uint32_t)kBufWord3};
+}
 
 // x / d for 0 <= x < 2^21, inv = 1 / d: the half keeps the product off every border
 __device__ __forceinline__ int quotient(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
@@ -82,7 +87,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   constexpr int NL = kHalf ? 1 : NC / kThreads;   // loads of a thread for a unit of K or V
   constexpr int PER = kHalf ? 1 : 2 * NL;         // loads of a thread for a unit
   static_assert(kHalf ? NC == kThreads / 2 : NC % kThreads == 0, "whole loads per thread");
-  typedef Ring<D> R;
+  constexpr int UB = kUnit * D * 2;          // bytes of a unit
+  __shared__ __attribute__((aligned(4 * UB))) char g_k[4 * UB];   // the rings (aligned: addresses in them are xored)
+  __shared__ __attribute__((aligned(4 * UB))) char g_v[4 * UB];
   __shared__ uint64_t s_mask[kDraftRows][2];   // masks of the rows' nodes (workgroups that reach the tree)
   __shared__ int s_row[kDraftRows];            // output rows
 
@@ -114,10 +121,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const bool lv = kHalf && wave >= 4;
   const long start = (long)u0 * kUnit * rs + (long)hkv * D;
   const uint32_t bytes = (uint32_t)(min((u1 - u0) * kUnit, len + n - u0 * kUnit) * rs * 2 - (rs - D) * 2);
-  const __amdgpu_buffer_rsrc_t kres =
-      __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_cache + start), 0, bytes, kBufWord3);
-  const __amdgpu_buffer_rsrc_t vres =
-      __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_cache + start), 0, bytes, kBufWord3);
+  const u32x4 kres = buffer_of(a.k_cache + start, bytes), vres = buffer_of(a.v_cache + start, bytes);
   uint32_t koff, voff;   // of the next unit to load
   {
     const int ltid = kHalf ? tid & (kThreads / 2 - 1) : tid;
@@ -126,22 +130,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     voff = (uint32_t)(lrow * rs * 2 + (lc ^ (2 * (lrow & VSWZ))) * 16);
   }
   const uint32_t unit_bytes = (uint32_t)(kUnit * rs * 2);
-  auto dma = [&](const __amdgpu_buffer_rsrc_t res, uint32_t& off, char* dst) __attribute__((always_inline)) {
+  const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_void*)g_k + lwave * 1024;
+  const uint32_t lds_v = (uint32_t)(uintptr_t)(lds_void*)g_v + lwave * 1024;
+  auto load_k = [&](int place) __attribute__((always_inline)) {
+    if (lv) return;
 #pragma unroll
-    for (int i = 0; i < NL; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (lds_void*)(dst + (i * kThreads + lwave * 64) * 16), 16, off,
-                                               i * LR * rs * 2, 0, 0);
-    off += unit_bytes;
+    for (int i = 0; i < NL; ++i) dma_lds(lds_k + place * UB + i * kThreads * 16, koff, kres, i * LR * rs * 2);
+    koff += unit_bytes;
   };
-  auto load_k = [&](auto bc) __attribute__((always_inline)) {
-    if (!lv) dma(kres, koff, R::k(decltype(bc)::value));
-  };
-  auto load_v = [&](auto bc) __attribute__((always_inline)) {
-    if (!kHalf || lv) dma(vres, voff, R::v(decltype(bc)::value));
+  auto load_v = [&](int place) __attribute__((always_inline)) {
+    if (kHalf && !lv) return;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) dma_lds(lds_v + place * UB + i * kThreads * 16, voff, vres, i * LR * rs * 2);
+    voff += unit_bytes;
   };
 
   // the first units are asked for before anything else; Q is waited for with the first of them
-  load_k(IntC<0>{});
+  load_k(0);
   const int rows_total = n * G;
   const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
   // Q's rows are read a line at a time (four parts of a row, 64 / LPR rows a load) and go
@@ -167,13 +172,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int i = 0; i < QL; ++i) w[b * QL + i] = *(const u32x4*)(from[i] + b * (D / 4));
     if (u1 * kUnit > len) mask = a.seen.m[node][hl];
   }
-  load_v(IntC<0>{});
-  load_k(IntC<1>{});
-  load_v(IntC<1>{});
-  load_k(IntC<2>{});
+  load_v(0);
+  load_k(1);
+  load_v(1);
+  load_k(2);
   if (busy) {
     if (u1 * kUnit > len) s_mask[wave * 32 + col][hl] = mask;
-    char* const mine = wave < 4 ? R::k(3) + wave * (8 * D) * 2 : R::v(3) + (wave - 4) * (8 * D) * 2;
+    char* const mine = (wave < 4 ? g_k : g_v) + 3 * UB + (wave & 3) * (UB / 4);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       asm volatile("" ::: "memory");
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
   float m_run = -__builtin_inff(), l_run = 0.f;
   const float c2 = a.scale_log2;
-  bool big = false;
+  float big = 0.f;   // largest |v| met
 
   // transposing reads of V (see pv below): block db of 32 dims lies at this address ^ 64 db (256
   // bytes on for each four blocks)
@@ -206,10 +211,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int i = lane & 15, g = lane >> 4;
     const int row = 4 * (g >> 1) + (i >> 2);
     const int c0 = 2 * (g & 1) + ((i & 3) >> 1);
-    vaddr = (uint32_t)(row * D * 2 + ((c0 ^ (2 * (row & VSWZ))) * 16) + (i & 1) * 8);
+    vaddr = (uint32_t)(uintptr_t)(lds_void*)g_v + (uint32_t)(row * D * 2 + ((c0 ^ (2 * (row & VSWZ))) * 16) + (i & 1) * 8);
   }
   // K row `col`, chunk hl ^ (col mod 16); chunk 2 s + hl is this address ^ 32 s
-  const uint32_t kaddr = (uint32_t)(col * D * 2 + ((hl ^ (col & KSWZ)) * 16));
+  const uint32_t kaddr = (uint32_t)(uintptr_t)(lds_void*)g_k + (uint32_t)(col * D * 2 + ((hl ^ (col & KSWZ)) * 16));
 
   // (what is derived from these is formed per unit: hoisted, it would cost registers)
   auto fresh = [](uint32_t x) __attribute__((always_inline)) -> uint32_t {
@@ -217,27 +222,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     return x;
   };
 
-  // ---- this thread's loads up to V of unit u and K of the next have landed (two units of
-  // loads are newer); its chunks of V to f16, in place
-  auto to_f16 = [&](auto bc) __attribute__((always_inline)) {
-    constexpr int B = decltype(bc)::value;
+  // ---- this thread's loads up to V of the unit in `place` and K of the next have landed (two
+  // units of loads are newer); its chunks of that V to f16, in place
+  auto to_f16 = [&](int place) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));
     asm volatile("" ::: "memory");
     if (kHalf && !lv) return;
+    u32x4* const at = (u32x4*)(g_v + place * UB + (fresh(tid) & (kHalf ? kThreads / 2 - 1 : kThreads - 1)) * 16);
+    u32x4 w[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) w[i] = at[i * kThreads];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      u32x4* at = (u32x4*)(R::v(B) + (i * kThreads + (fresh(tid) & (kHalf ? kThreads / 2 - 1 : kThreads - 1))) * 16);
-      const u32x4 w = *at;
       f16x8 x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xFFFF0000u);
-        big |= !(fabsf(lo) < 65536.f) | !(fabsf(hi) < 65536.f);
+        const float lo = __uint_as_float(w[i][e] << 16), hi = __uint_as_float(w[i][e] & 0xFFFF0000u);
+        big = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), big);
         x[2 * e] = (_Float16)lo;
         x[2 * e + 1] = (_Float16)hi;
       }
-      *at = __builtin_bit_cast(u32x4, x);
+      at[i * kThreads] = __builtin_bit_cast(u32x4, x);
     }
+    asm volatile("" : "+v"(big));   // here, not behind the next products with the values kept until then
   };
 
   f32x16 sacc;
@@ -257,32 +264,34 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
     }
   };
-  auto pv = [&](const char* vs) __attribute__((always_inline)) {
-    const uint32_t vx = fresh(vaddr);
+  auto pv = [&](int place) __attribute__((always_inline)) {
+    const uint32_t vx = vaddr + place * UB;
+    // lane group g reads keys 4 (g >> 1) + 0 .. 3 (+ 16 k16, + 8) at dims 32 db + 16 (g & 1) .. ;
+    // the blocks that share an address follow one another
 #pragma unroll
-    for (int k16 = 0; k16 < 2; ++k16) {
+    for (int lo = 0; lo < (NDB < 4 ? NDB : 4); ++lo)
 #pragma unroll
-      for (int db = 0; db < NDB; ++db) {
-        // lane group g reads keys 4 (g >> 1) + 0 .. 3 (+ 16 k16, + 8) at dims 32 db + 16 (g & 1) ..
-        const char* at = vs + (vx ^ (64 * (db & 3))) + (db >> 2) * 256 + 16 * k16 * D * 2;
-        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * D * 2));
-        const u32x2 w0 = __builtin_bit_cast(u32x2, x0), w1 = __builtin_bit_cast(u32x2, x1);
-        const f16x8 va = __builtin_bit_cast(f16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pf[k16], o[db], 0, 0, 0);
-      }
-    }
+      for (int k16 = 0; k16 < 2; ++k16)
+#pragma unroll
+        for (int db = lo; db < NDB; db += 4) {
+          const uint32_t at = (vx ^ (64 * lo)) + (db >> 2) * 256 + 16 * k16 * D * 2;
+          const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+          const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 8 * D * 2));
+          const u32x2 w0 = __builtin_bit_cast(u32x2, x0), w1 = __builtin_bit_cast(u32x2, x1);
+          const f16x8 va = __builtin_bit_cast(f16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pf[k16], o[db], 0, 0, 0);
+        }
     sched_reads(IntC<2 * NDB>{}, IntC<2>{});
   };
-  auto qk = [&](auto bc) __attribute__((always_inline)) {
-    constexpr int B = decltype(bc)::value;
-    const char* ks = R::k(B);
-    const uint32_t kx = fresh(kaddr);
+  auto qk = [&](int place) __attribute__((always_inline)) {
+    const uint32_t kx = kaddr + place * UB;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sacc[e] = 0.f;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const bf16x8 ka = __builtin_bit_cast(bf16x8, *(const u32x4*)(ks + (kx ^ (32 * s & 16 * KSWZ)) + (32 * s & ~(16 * KSWZ))));
+    for (int i = 0; i < NS; ++i) {
+      const int s = NS == 16 ? (i >> 1) + 8 * (i & 1) : i;   // steps that share an address follow one another
+      const bf16x8 ka = __builtin_bit_cast(
+          bf16x8, *(const lds_u32x4*)(uintptr_t)((kx ^ (32 * s & 16 * KSWZ)) + (32 * s & ~(16 * KSWZ))));
       sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[s], sacc, 0, 0, 0);
     }
     sched_reads(IntC<NS>{}, IntC<1>{});
@@ -329,55 +338,55 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
   };
 
-  // Unit u in ring place B. K of unit u - 1 and V of unit u - 2 are no longer read after the
-  // first barrier: their places take units u + 3 and u + 2.
-  auto refill = [&](auto bc) __attribute__((always_inline)) {
-    constexpr int B = decltype(bc)::value;
-    load_k(IntC<(B + 3) & 3>{});
-    load_v(IntC<(B + 2) & 3>{});
+  // ---- half-steps, a barrier before each: in half-step 2 t waves 0 - 3 form the products of unit
+  // t while waves 4 - 7 run the softmax of unit t - 1, in 2 t + 1 the other way round. K of
+  // unit t - 1 and V of unit t - 2 are no longer read from 2 t on: their places take units t + 3
+  // and t + 2. V of unit t is turned to f16 in 2 t and 2 t + 1 and first read in 2 t + 2.
+  const int n_units = u1 - u0;
+  constexpr int UNR = 2;
+  auto refill = [&](int t) __attribute__((always_inline)) {
+    load_k((t + 3) & 3);
+    load_v((t + 2) & 3);
   };
-  auto early = [&](auto bc, int u) __attribute__((always_inline)) {   // waves 0 - 3
-    constexpr int B = decltype(bc)::value;
+  auto early = [&](int t) __attribute__((always_inline)) {   // waves 0 - 3
     wg_barrier();
-    refill(bc);
+    refill(t);
     if (busy) {
-      if (u > u0) pv(R::v((B + 3) & 3));
-      qk(bc);
+      if (t > 0) pv((t - 1) & 3);
+      qk(t & 3);
     }
     wg_barrier();
-    if (busy) softmax(u);
-    to_f16(bc);
+    if (busy) softmax(u0 + t);
+    to_f16(t & 3);
   };
-  auto late = [&](auto bc, int u) __attribute__((always_inline)) {    // waves 4 - 7
-    constexpr int B = decltype(bc)::value;
+  auto later = [&](int t) __attribute__((always_inline)) {   // waves 4 - 7
     wg_barrier();
-    refill(bc);
-    if (busy && u > u0) softmax(u - 1);
-    to_f16(bc);
+    refill(t);
+    if (busy && t > 0) softmax(u0 + t - 1);
+    to_f16(t & 3);
     wg_barrier();
     if (busy) {
-      if (u > u0) pv(R::v((B + 3) & 3));
-      qk(bc);
+      if (t > 0) pv((t - 1) & 3);
+      qk(t & 3);
     }
   };
   auto run = [&](auto step) __attribute__((always_inline)) {
-    for (int u = u0; u < u1; u += 4) {
-      step(IntC<0>{}, u);
-      if (u + 1 < u1) step(IntC<1>{}, u + 1);
-      if (u + 2 < u1) step(IntC<2>{}, u + 2);
-      if (u + 3 < u1) step(IntC<3>{}, u + 3);
+    for (int t = 0; t < n_units; t += UNR) {
+#pragma unroll
+      for (int i = 0; i < UNR; ++i)
+        if (i == 0 || t + i < n_units) step(t + i);
     }
   };
   __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));   // K of the first unit
   if (wave < 4) run(early);
-  else run(late);
+  else run(later);
   __builtin_amdgcn_s_waitcnt(vm_wait(0));   // the loads past the split's end: no write into LDS may come later
   wg_barrier();
   if (busy) {
     if (wave >= 4) softmax(u1 - 1);
-    pv(R::v((u1 - 1 - u0) & 3));   // no load is in flight: the place may be any
+    pv((n_units - 1) & 3);
   }
-  if (big) status_raise(a.status, kFaultRange);
+  if (big >= 65520.f) status_raise(a.status, kFaultRange);
   wg_barrier();   // the rings are written over below
   if (!busy) return;
   const uint32_t te = fresh(tid);
@@ -395,7 +404,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     ml[1] = l_tot;
   }
   // the wave's 32 rows through its own place of the rings, then 16 bytes a lane in whole rows
-  char* const mine = wave < 4 ? R::k(wave) : R::v(wave - 4);
+  char* const mine = (wave < 4 ? g_k : g_v) + (wave & 3) * UB;
 #pragma unroll
   for (int db = 0; db < NDB; ++db)
 #pragma unroll
