@@ -404,25 +404,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     ml[1] = l_tot;
   }
   // the wave's 32 rows through its own place of the rings, then 16 bytes a lane in whole rows
-  char* const mine = (wave < 4 ? g_k : g_v) + (wave & 3) * UB;
+  const uint32_t mine = (uint32_t)(uintptr_t)(lds_void*)(wave < 4 ? g_k : g_v) + (wave & 3) * UB;
+  const uint32_t wr = mine + col_e * D * 2 + hl_e * 8 + (col_e & KSWZ) * 16;
+  auto rows_out = [&](auto type) __attribute__((always_inline)) {
+    typedef decltype(type) vec4;
 #pragma unroll
-  for (int db = 0; db < NDB; ++db)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      char* at = mine + col_e * D * 2 + (((4 * db + i) ^ (col_e & KSWZ)) * 16) + hl_e * 8;
-      const float x0 = o[db][4 * i] * inv, x1 = o[db][4 * i + 1] * inv, x2 = o[db][4 * i + 2] * inv, x3 = o[db][4 * i + 3] * inv;
-      if (whole) *(bf16x4*)at = bf16x4{(__bf16)x0, (__bf16)x1, (__bf16)x2, (__bf16)x3};
-      else *(f16x4*)at = f16x4{(_Float16)x0, (_Float16)x1, (_Float16)x2, (_Float16)x3};
+    for (int c = 0; c < 4 * NDB; ++c) {
+      const int db = c >> 2, i = c & 3;
+      const f32x4 x = f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]} * inv;
+      *(__attribute__((address_space(3))) vec4*)(uintptr_t)((wr ^ (16 * c & 16 * KSWZ)) + (16 * c & ~(16 * KSWZ))) =
+          __builtin_convertvector(x, vec4);
     }
+  };
+  if (whole) rows_out(bf16x4{});
+  else rows_out(f16x4{});
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(kLgkmWait0);
-  char* const to = whole ? (char*)a.out : (char*)(a.part_o + (long)split * n * Hq * D);
+  // rows past the last (s_row is -1) lie past the resource: their stores are dropped
+  const __amdgpu_buffer_rsrc_t out_res = __builtin_amdgcn_make_buffer_rsrc(
+      whole ? (void*)a.out : (void*)(a.part_o + (long)split * n * Hq * D), 0, n * Hq * D * 2, kBufWord3);
 #pragma unroll
   for (int i = 0; i < kUnit * RC / 64; ++i) {
     const int q = i * 64 + lane_e, rr = q / RC, c = q % RC;
-    const u32x4 x = *(const u32x4*)(mine + rr * D * 2 + ((c ^ (rr & KSWZ)) * 16));
-    const int orow = s_row[wave * 32 + rr];
-    if (orow >= 0) *(u32x4*)(to + ((long)orow * D + 8 * c) * 2) = x;
+    const u32x4 x = *(const lds_u32x4*)(uintptr_t)(mine + rr * D * 2 + ((c ^ (rr & KSWZ)) * 16));
+    __builtin_amdgcn_raw_buffer_store_b128(x, out_res, s_row[wave * 32 + rr] * (D * 2) + c * 16, 0, 0);
   }
 }
 
