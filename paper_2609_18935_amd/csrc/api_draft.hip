@@ -106,8 +106,7 @@ size_t attention_ws(const tu_attn_params* p, int64_t n, int splits) {
   return kStatusBytes + align_up(rows * p->head_dim * sizeof(_Float16)) + align_up(rows * 2 * sizeof(float));
 }
 
-constexpr size_t kVerifyBytes = kStatusBytes + ((kMaxDraft + 1) * sizeof(int32_t) + kAlign - 1) / kAlign * kAlign +
-                                (kMaxDraft + 1) * kDrawMaxBlocks * sizeof(double);
+constexpr size_t kVerifyBytes = kStatusBytes + (kMaxDraft + 1) * kDrawMaxBlocks * sizeof(double);
 
 int check_workspace(const void* ws, size_t bytes, size_t need) {
   if (!ws || bytes < need) return fail(TU_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", bytes, need);
@@ -383,14 +382,26 @@ int draft_verify(const tu_draft* draft, const int32_t* tokens, const float* targ
     a.proposal_stride = proposal_stride;
     a.vocab = vocab;
     Arena ar(after_status(workspace));
-    a.arrived = static_cast<int32_t*>(ar.take((kMaxDraft + 1) * sizeof(int32_t)));
-    a.part = static_cast<double*>(ar.take((kMaxDraft + 1) * kDrawMaxBlocks * sizeof(double)));
+    a.part = static_cast<unsigned long long*>(ar.take((kMaxDraft + 1) * kDrawMaxBlocks * sizeof(double)));
     a.status = call_status(workspace);
     a.n = n;
-    const int64_t per_block = kDrawThreads * kDrawPer;
-    a.n_blocks = (int32_t)std::min<int64_t>(kDrawMaxBlocks, (vocab + per_block - 1) / per_block);
-    a.slice = (vocab + a.n_blocks - 1) / a.n_blocks;
-    for (int i = 0; i < n; ++i) a.parent[i] = (int16_t)draft->parent[i];
+    // as few whole blocks of a workgroup's elements a slice as kDrawMaxBlocks slices allow
+    const int64_t block = kDrawThreads * kDrawPer, blocks = (vocab + block - 1) / block;
+    a.slice = (blocks + kDrawMaxBlocks - 1) / kDrawMaxBlocks * block;
+    a.n_blocks = (int32_t)((vocab + a.slice - 1) / a.slice);
+    a.wide = ((uintptr_t)target & 15) == 0 && target_stride % 4 == 0 &&
+             (!proposal || (((uintptr_t)proposal & 15) == 0 && proposal_stride % 4 == 0));
+    uint8_t last[kMaxDraft] = {};    // last child so far
+    for (int i = 1; i < n; ++i) {
+      const int up = draft->parent[i];
+      a.parent[i] = (uint8_t)up;
+      if (last[up]) a.sibling[last[up]] = (uint8_t)i;
+      else {
+        a.child[up] = (uint8_t)i;
+        a.first[i >> 6] |= 1ull << (i & 63);
+      }
+      last[up] = (uint8_t)i;
+    }
     draft_masks(draft, &a.seen);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (int e = hip_check(timed("draft_verify", st, [&] { return launch_draft_clear(a, st); }), "draft verification")) return e;

@@ -90,7 +90,7 @@ struct DraftDeltaArgs {
 };
 
 constexpr int kDrawThreads = 512;
-constexpr int kDrawPer = 8;       // row elements of a thread that stay in registers
+constexpr int kDrawPer = 8;       // consecutive row elements of a thread, in registers
 constexpr int kDrawMaxBlocks = 64;
 struct DraftVerifyArgs {
   const int32_t* tokens;
@@ -101,13 +101,17 @@ struct DraftVerifyArgs {
   int64_t target_stride;
   int64_t proposal_stride;
   int64_t vocab;
-  int32_t* arrived;         // [kMaxDraft + 1] workgroups that have written their part of a pass
-  double* part;             // [kMaxDraft + 1][kDrawMaxBlocks] partial sums
+  unsigned long long* part; // [n + 1][n_blocks] sums of the passes (bits of a double)
   CallStatus status;
   int32_t n;
   int32_t n_blocks;         // workgroups of a pass, each a contiguous slice of the row
-  int64_t slice;            // elements of a slice
-  int16_t parent[kMaxDraft];
+  int64_t slice;            // elements of a slice, a multiple of kDrawThreads * kDrawPer
+  int32_t wide;             // every row is 16-byte aligned
+  int32_t pad;
+  uint64_t first[2];        // nodes that are their parent's first child
+  uint8_t parent[kMaxDraft];
+  uint8_t child[kMaxDraft];    // first child (0: none)
+  uint8_t sibling[kMaxDraft];  // next child of the same parent (0: none)
   DraftMasks seen;
 };
 

@@ -7,13 +7,16 @@
 // an acceptance of a first child nothing. (A drafter's choice without probabilities is a
 // point mass: the rejected tokens' entries are zero instead.)
 //
-// k_draft_clear (one workgroup) zeroes the counters of the passes. k_draft_draw: every
-// workgroup reads the single probabilities that the tests need, of all nodes at once, and
-// derives the same walk from them; where a node has a rejection, or no child is left to try,
-// each sums its slice of the row in float64, publishes the sum, waits for the others
-// (bounded; the few workgroups fit the chip many times over), and adds all of them up in one
-// order. The workgroup whose slice holds the drawn token finds it. Bound by the latency of the
-// passes; the rows themselves (a megabyte) are read once and stay in registers.
+// k_draft_clear empties the places of the passes' sums. k_draft_draw: every workgroup reads the
+// single probabilities that the tests need, of all nodes at once, and derives the same walk
+// from them; where a node has a rejection, or no child is left to try, each sums its slice of
+// the row in float64 and publishes the sum, reads the others' as they appear (a bounded wait;
+// the few workgroups fit the chip many times over) and adds all of them up in one order. The
+// workgroup whose slice holds the drawn token finds it. Bound by latency: the odds (two
+// dependent loads), the rows of a node (a load; a megabyte, kept in registers over its passes)
+// and one exchange a pass.
+#include <algorithm>
+
 #include "draft.h"
 
 namespace tu {
@@ -21,7 +24,8 @@ namespace tu {
 namespace {
 
 constexpr long kSpinLimit = 1l << 20;   // polls of a bounded wait
-constexpr int kClearThreads = kMaxDraft;
+constexpr int kClearThreads = 256;
+static_assert(kDrawMaxBlocks == 64, "a slice's sum per lane");
 constexpr int kWaves = kDrawThreads / 64;
 
 // What the tests of node i (as a child of its parent) need of the rows.
@@ -32,8 +36,8 @@ struct Odds {
 
 __device__ __forceinline__ Odds odds_of(const DraftVerifyArgs& a, int i) {
   Odds o{0.f, 1.f, 2.f, -1};
-  const int up = i > 0 && i < a.n ? a.parent[i] : -1;
-  if (up < 0) return o;
+  if (i == 0) return o;
+  const int up = a.parent[i];
   const int x = a.tokens[i];
   o.u = a.u[i];
   if (x < 0 || x >= a.vocab) return o;
@@ -43,48 +47,70 @@ __device__ __forceinline__ Odds odds_of(const DraftVerifyArgs& a, int i) {
   return o;
 }
 
+// A sum that has not been written yet. (A sum that is not a number is written as another NaN.)
+constexpr unsigned long long kEmpty = ~0ull;
+
 __global__ __launch_bounds__(kClearThreads) void k_draft_clear(DraftVerifyArgs a) {
   status_mark(a.status);
-  for (int i = threadIdx.x; i <= kMaxDraft; i += kClearThreads) a.arrived[i] = 0;
-  for (int i = threadIdx.x; i < a.n + 2; i += kClearThreads) a.result[i] = i == 0 ? 0 : -1;
+  const int t = blockIdx.x * kClearThreads + threadIdx.x;
+  for (int i = t; i < (a.n + 1) * a.n_blocks; i += gridDim.x * kClearThreads) a.part[i] = kEmpty;
+  if (t < a.n + 2) a.result[t] = t == 0 ? 0 : -1;
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
+// x + the sums of the lanes before it
+__device__ __forceinline__ double wave_scan(double x, int lane) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
+  for (int d = 1; d < 64; d <<= 1) {
+    const double y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
   return x;
+}
+
+// 8 elements of a row from t on (0 past its end); `wide`: the address is a multiple of 16
+__device__ __forceinline__ void load_row(const float* row, int64_t t, int64_t hi, bool wide, float (&x)[kDrawPer]) {
+  static_assert(kDrawPer == 8, "two vectors");
+  if (wide && t + kDrawPer <= hi) {
+    *(f32x4*)x = *(const f32x4*)(row + t);
+    *(f32x4*)(x + 4) = *(const f32x4*)(row + t + 4);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kDrawPer; ++j) x[j] = t + j < hi ? row[t + j] : 0.f;
+  }
 }
 
 __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) {
   __shared__ Odds s_odds[kMaxDraft];
   __shared__ uint64_t s_seen[kMaxDraft][2];
-  __shared__ int s_parent[kMaxDraft];
+  __shared__ uint8_t s_child[kMaxDraft], s_sibling[kMaxDraft];
   __shared__ unsigned long long s_first[2], s_on[2];   // accepted as first children; on the accepted path
-  __shared__ double s_wave[kWaves];
-  __shared__ double s_part[kDrawMaxBlocks];
+  __shared__ double s_wave[kWaves], s_before[kDrawMaxBlocks + 1];   // sums of the waves; of the slices before a slice
   __shared__ int s_out[kMaxDraft];                     // rejected tokens of the row (point-mass drafts)
   __shared__ int s_mine[kMaxDraft];                    // those of this workgroup's slice
-  __shared__ int s_found, s_best, s_expired;
+  __shared__ int s_last, s_expired;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = a.n, blk = blockIdx.x;
   const bool drawn = a.proposal != nullptr;
 
   if (tid < 2) s_first[tid] = 0;
   if (tid == 0) s_expired = 0;
+  if (tid < n) {
+    s_seen[tid][0] = a.seen.m[tid][0];
+    s_seen[tid][1] = a.seen.m[tid][1];
+    s_child[tid] = a.child[tid];
+    s_sibling[tid] = a.sibling[tid];
+  }
   __syncthreads();
   if (tid < n) {
     const Odds o = odds_of(a, tid);
     s_odds[tid] = o;
-    s_seen[tid][0] = a.seen.m[tid][0];
-    s_seen[tid][1] = a.seen.m[tid][1];
-    s_parent[tid] = a.parent[tid];
-    bool first = true;   // the first child of its parent
-    for (int j = 1; j < tid; ++j) first &= a.parent[j] != a.parent[tid];
+    const bool first = a.first[tid >> 6] >> (tid & 63) & 1;   // the first child of its parent
     if (tid == 0 || (first && (double)o.u * (double)o.q < (double)o.p)) atomicOr(&s_first[tid >> 6], 1ull << (tid & 63));
   }
-  __syncthreads();
 
   const int64_t lo = min(a.vocab, (int64_t)blk * a.slice), hi = min(a.vocab, lo + a.slice);
+  const int64_t t0 = lo + tid * kDrawPer;      // this thread's elements of the slice's first block
+  const bool wide = a.wide;
   int pass = 0;
   for (;;) {
     // the deepest node all of whose ancestors (and itself) are accepted
@@ -96,13 +122,9 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
     const int m = s_on[1] ? 127 - __builtin_clzll(s_on[1]) : 63 - __builtin_clzll(s_on[0]);
     const float* P = a.target + m * a.target_stride;
     const float* Q = drawn ? a.proposal + m * a.proposal_stride : nullptr;
-    float pr[kDrawPer], qr[kDrawPer];
-#pragma unroll
-    for (int j = 0; j < kDrawPer; ++j) {
-      const int64_t t = lo + (int64_t)j * kDrawThreads + tid;
-      pr[j] = t < hi ? P[t] : 0.f;
-      qr[j] = drawn && t < hi ? Q[t] : 0.f;
-    }
+    float pr[kDrawPer], qr[kDrawPer] = {};
+    load_row(P, t0, hi, wide, pr);
+    if (drawn) load_row(Q, t0, hi, wide, qr);
 
     double b = 0.0, F = 1.0;
     int n_out = 0, n_mine = 0;
@@ -116,46 +138,60 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
         if (out[k] == t) return 0.0;
       return p > 0.f ? (double)p : 0.0;
     };
-    // sum of what is left over the whole row, the same in every workgroup
-    auto total = [&]() -> double {
+    // this thread's part of block t - lo of the slice, in element order
+    auto block_sum = [&](const float (&p)[kDrawPer], const float (&q)[kDrawPer], int64_t t) __attribute__((always_inline)) -> double {
       double x = 0.0;
 #pragma unroll
-      for (int j = 0; j < kDrawPer; ++j) x += left(pr[j], qr[j], lo + (int64_t)j * kDrawThreads + tid, s_mine, n_mine);
-      for (int64_t t = lo + (int64_t)kDrawPer * kDrawThreads + tid; t < hi; t += kDrawThreads)
-        x += left(P[t], drawn ? Q[t] : 0.f, t, s_mine, n_mine);
-      x = wave_sum(x);
+      for (int j = 0; j < kDrawPer; ++j) x += left(p[j], q[j], t + j, s_mine, n_mine);
+      return x;
+    };
+    // sum of what is left over the whole row, the same in every workgroup
+    auto total = [&]() -> double {
+      double x = block_sum(pr, qr, t0);
+      for (int64_t t = t0 + kDrawThreads * kDrawPer; t < hi; t += kDrawThreads * kDrawPer) {
+        float p[kDrawPer], q[kDrawPer] = {};
+        load_row(P, t, hi, wide, p);
+        if (drawn) load_row(Q, t, hi, wide, q);
+        x += block_sum(p, q, t);
+      }
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
       if (lane == 0) s_wave[wave] = x;
       __syncthreads();
-      if (tid == 0) {
-        double sum = 0.0;
-        for (int w = 0; w < kWaves; ++w) sum += s_wave[w];
-        double* slot = a.part + (int64_t)pass * kDrawMaxBlocks + blk;
-        __hip_atomic_store(slot, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_fetch_add(a.arrived + pass, 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
+      if (wave == 0) {
+        unsigned long long* slots = a.part + (int64_t)pass * a.n_blocks;
+        if (lane == 0) {
+          double sum = 0.0;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) sum += s_wave[w];
+          const unsigned long long bits = sum == sum ? __builtin_bit_cast(unsigned long long, sum) : 0x7ff8000000000000ull;
+          __hip_atomic_store(slots + blk, bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        unsigned long long bits = 0;   // slices past the last are empty: 0.0
         long spins = 0;
-        while (__hip_atomic_load(a.arrived + pass, __ATOMIC_ACQUIRE, __HIP_MEMORY_SCOPE_AGENT) < a.n_blocks) {
-          __builtin_amdgcn_s_sleep(1);
+        for (;;) {
+          if (lane < a.n_blocks) bits = __hip_atomic_load(slots + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          if (__all(bits != kEmpty)) break;
           if (++spins > kSpinLimit) {
             s_expired = 1;
             break;
           }
         }
+        const double mine = __builtin_bit_cast(double, bits);
+        const double upto = wave_scan(mine, lane);
+        if (lane < kDrawMaxBlocks) s_before[lane + 1] = upto;
+        if (lane == 0) s_before[0] = 0.0;
+        const uint64_t some = __ballot(mine > 0.0);
+        if (lane == 0) s_last = some ? 63 - __builtin_clzll(some) : -1;   // the last slice with a share
       }
       __syncthreads();
-      if (tid < a.n_blocks)
-        s_part[tid] = __hip_atomic_load(a.part + (int64_t)pass * kDrawMaxBlocks + tid, __ATOMIC_RELAXED,
-                                        __HIP_MEMORY_SCOPE_AGENT);
-      __syncthreads();
-      double sum = 0.0;
-      for (int w = 0; w < a.n_blocks; ++w) sum += s_part[w];
       ++pass;
-      return sum;
+      return s_before[kDrawMaxBlocks];
     };
 
     int took = -1;
     bool tried = false;
-    for (int c = m + 1; c < n && took < 0; ++c) {
-      if (s_parent[c] != m) continue;
+    for (int c = s_child[m]; c > 0 && took < 0; c = s_sibling[c]) {
       const Odds o = s_odds[c];
       double px = 0.0;
       if (o.token >= 0) px = left(o.p, o.q, o.token, s_out, n_out);
@@ -194,58 +230,74 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
       F = total();
     }
     if (s_expired) break;
-    if (blk == 0 && tid == 0) {
-      int k = 0;
-      for (int i = 0; i < n; ++i)
-        if (s_on[i >> 6] >> (i & 63) & 1) a.result[2 + k++] = i;
-      a.result[0] = k;
+    if (blk == 0 && tid < n && (s_on[tid >> 6] >> (tid & 63) & 1)) {   // the path, in order
+      const uint64_t below = (1ull << (tid & 63)) - 1;
+      const int at = __popcll(s_on[0] & (tid < 64 ? below : ~0ull)) + (tid < 64 ? 0 : __popcll(s_on[1] & below));
+      a.result[2 + at] = tid;
+      if (tid == m) a.result[0] = at + 1;
     }
+    if (!(F > 0.0 && F < __builtin_inf())) break;   // no distribution: no token
     // the slice that holds the drawn token: the first whose cumulative sum exceeds the target
+    // (the last one with a share if u[0] times the whole was rounded up to the whole)
     const double want = (double)a.u[0] * F;
-    double before = 0.0;
-    int owner = -1, last = -1;
-    for (int w = 0; w < a.n_blocks && owner < 0; ++w) {
-      if (s_part[w] > 0.0) last = w;
-      if (before + s_part[w] > want) owner = w;
-      else before += s_part[w];
-    }
-    const bool rounded = owner < 0;          // u[0] times the whole rounded up to the whole
-    if (rounded) owner = last;
-    if (owner == blk && F > 0.0 && F < __builtin_inf()) {
-      if (tid == 0) {
-        s_found = 0x7fffffff;
-        s_best = -1;
+    int owner = s_last;
+    for (int w = 0; w < a.n_blocks; ++w)
+      if (s_before[w + 1] > want) {
+        owner = w;
+        break;
       }
-      __syncthreads();
-      int best = -1;                         // the last element with a share, should none exceed
-      for (int64_t t0 = lo; t0 < hi; t0 += kDrawThreads) {
-        const int64_t t = t0 + tid;
-        const double x = t < hi ? left(P[t], drawn ? Q[t] : 0.f, t, s_mine, n_mine) : 0.0;
-        if (x > 0.0) best = (int)t;
-        double cum = x;                      // inclusive sum within the wave
+    if (owner != blk) break;
+    double before = s_before[blk];
+    int found = -1;
+    for (int64_t tb = lo; tb < hi; tb += kDrawThreads * kDrawPer) {
+      const int64_t t = tb + tid * kDrawPer;
+      float p[kDrawPer], q[kDrawPer] = {};
+      if (tb == lo) {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const double y = __shfl_up(cum, d, 64);
-          if (lane >= d) cum += y;
-        }
-        if (lane == 63) s_wave[wave] = cum;
-        __syncthreads();
-        double base = before, all = before;
-        for (int w = 0; w < kWaves; ++w) {
-          if (w < wave) base += s_wave[w];
-          all += s_wave[w];
-        }
-        if (!rounded && x > 0.0 && base + cum > want) atomicMin(&s_found, (int)t);
-        before = all;
-        __syncthreads();
-        const int found = s_found;
-        __syncthreads();
-        if (found != 0x7fffffff) break;
+        for (int j = 0; j < kDrawPer; ++j) p[j] = pr[j], q[j] = qr[j];
+      } else {
+        load_row(P, t, hi, wide, p);
+        if (drawn) load_row(Q, t, hi, wide, q);
       }
-      if (s_found == 0x7fffffff) atomicMax(&s_best, best);
+      const double x = block_sum(p, q, t);
+      const double cum = wave_scan(x, lane);
       __syncthreads();
-      if (tid == 0) a.result[1] = s_found == 0x7fffffff ? s_best : s_found;
+      if (lane == 63) s_wave[wave] = cum;
+      __syncthreads();
+      double base = before;
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) base += s_wave[w];
+        before += s_wave[w];
+      }
+      // this thread's first element that takes the sum past the target, else its last with a share
+      double sum = base + (cum - x);
+      int first = -1, last = -1;
+#pragma unroll
+      for (int j = 0; j < kDrawPer; ++j) {
+        const double v = left(p[j], q[j], t + j, s_mine, n_mine);
+        sum += v;
+        if (v > 0.0) {
+          last = (int)(t + j);
+          if (first < 0 && sum > want) first = last;
+        }
+      }
+      // the first thread of the block that has one; the last thread with a share otherwise
+      __shared__ int s_pick[2][kWaves];
+      const uint64_t has = __ballot(first >= 0), share = __ballot(last >= 0);
+      if (has ? lane == __builtin_ctzll(has) : lane == 0) s_pick[0][wave] = has ? first : -1;
+      if (share ? lane == 63 - __builtin_clzll(share) : lane == 0) s_pick[1][wave] = share ? last : -1;
+      __syncthreads();
+      int hit = -1;
+      for (int w = kWaves - 1; w >= 0; --w) {
+        if (s_pick[0][w] >= 0) hit = s_pick[0][w];
+        found = max(found, s_pick[1][w]);
+      }
+      if (hit >= 0) {
+        found = hit;
+        break;
+      }
     }
+    if (tid == 0) a.result[1] = found;
     break;
   }
   if (tid == 0 && s_expired) status_raise(a.status, kFaultWait);
@@ -254,7 +306,8 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
 }  // namespace
 
 hipError_t launch_draft_clear(const DraftVerifyArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(k_draft_clear, dim3(1), dim3(kClearThreads), 0, s, a);
+  const int blocks = std::max(1, std::min(16, ((a.n + 1) * a.n_blocks + kClearThreads - 1) / kClearThreads));
+  hipLaunchKernelGGL(k_draft_clear, dim3(blocks), dim3(kClearThreads), 0, s, a);
   return hipGetLastError();
 }
 
