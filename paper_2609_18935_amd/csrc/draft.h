@@ -115,9 +115,9 @@ struct DraftVerifyArgs {
   DraftMasks seen;
 };
 
-constexpr int kMaxAcceptDelta = 32;
-constexpr int kMaxAcceptConv = 32;
-constexpr int kMaxAcceptBufs = 32;
+constexpr int kMaxAcceptDelta = 48;
+constexpr int kMaxAcceptConv = 48;
+constexpr int kMaxAcceptBufs = 64;
 struct AcceptDelta {
   float* state;
   const bf16_t* k;

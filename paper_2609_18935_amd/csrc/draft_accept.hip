@@ -2,8 +2,9 @@
 // delta layers' states and the convolutions' carried rows.
 //
 // Delta states: the recurrence token by token along the path, as k_delta_step without outputs:
-// a workgroup takes 16 rows of one value head, 16 lanes a row, the row in registers from the
-// first token to the last. Bound by HBM: each state is read and written once.
+// 16 lanes hold a row of one value head in registers from the first token to the last, two rows
+// at a time (two chains of dependent sums in flight, a token's operands read once for both).
+// Bound by HBM: each state is read and written once.
 //
 // Cache rows: a thread takes one 16-byte column of a K or V buffer and moves it row by row in
 // path order. Row len + j only ever overwrites rows whose own move came earlier (path[j] >= j,
@@ -19,8 +20,9 @@ namespace tu {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 16;
-constexpr int kLanes = kThreads / kRows;
+constexpr int kPairs = 16;             // row pairs of a workgroup
+constexpr int kRows = 2 * kPairs;
+constexpr int kLanes = kThreads / kPairs;
 constexpr int kBatch = 8;   // cache rows in flight
 
 template <int ROT>
@@ -42,44 +44,66 @@ __device__ __forceinline__ void advance(const AcceptArgs& a, int item) {
   const int h = rem / NSL, kh = h / (Hv / Hk);
   const int row = (rem - h * NSL) * kRows + threadIdx.x / kLanes, l = threadIdx.x % kLanes;
   const AcceptDelta L = a.delta[li];
-  float* sp = L.state + ((long)h * DK + row) * DK + NC * l;
-  float st[NC];
-#pragma unroll
-  for (int c = 0; c < NC; c += 4) {
-    const f32x4 x = *(const f32x4*)(sp + c);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) st[c + e] = x[e];
-  }
-  for (int j = 0; j < a.n_path; ++j) {
+  // a token's operands, requested a token ahead
+  struct Token {
+    uint32_t k[NC / 2];
+    uint32_t v[2];
+    float beta, g;
+  };
+  auto token = [&](int j) __attribute__((always_inline)) -> Token {
+    Token x;
     const long t = a.path[j];
     const bf16_t* kp = L.k + (t * Hk + kh) * DK + NC * l;
-    uint32_t w[NC / 2];
-    if constexpr (NC == 8) *(u32x4*)w = *(const u32x4*)kp;
-    else *(u32x2*)w = *(const u32x2*)kp;
+    if constexpr (NC == 8) *(u32x4*)x.k = *(const u32x4*)kp;
+    else *(u32x2*)x.k = *(const u32x2*)kp;
+    const bf16_t* vp = L.v + (t * Hv + h) * DK + row;
+    x.v[0] = vp[0];
+    x.v[1] = vp[kPairs];
+    x.beta = L.beta[t * Hv + h];
+    x.g = L.g[t * Hv + h];
+    return x;
+  };
+  float* sp = L.state + ((long)h * DK + row) * DK + NC * l;
+  float st[2][NC];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < NC; c += 4) {
+      const f32x4 x = *(const f32x4*)(sp + r * kPairs * DK + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st[r][c + e] = x[e];
+    }
+  Token now = token(0);
+  for (int j = 0; j < a.n_path; ++j) {
+    const Token next = token(min(j + 1, a.n_path - 1));
     float kf[NC];
 #pragma unroll
     for (int e = 0; e < NC / 2; ++e) {
-      kf[2 * e] = __uint_as_float(w[e] << 16);
-      kf[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+      kf[2 * e] = __uint_as_float(now.k[e] << 16);
+      kf[2 * e + 1] = __uint_as_float(now.k[e] & 0xFFFF0000u);
     }
-    const float v = bf16_to_f32(L.v[(t * Hv + h) * DK + row]);
-    const float beta = L.beta[t * Hv + h];
-    const float gin = L.g[t * Hv + h];
-    const float g = gin < 0x1p-100f ? 0x1p-100f : gin;
-    float d0 = 0.f, d1 = 0.f;
+    const float g = now.g < 0x1p-100f ? 0x1p-100f : now.g;
+    float d[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, u[2];
 #pragma unroll
-    for (int c = 0; c < NC; c += 2) {
-      st[c] *= g;
-      st[c + 1] *= g;
-      d0 = __builtin_fmaf(st[c], kf[c], d0);
-      d1 = __builtin_fmaf(st[c + 1], kf[c + 1], d1);
-    }
-    const float u = beta * (v - row_sum(d0 + d1));
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) st[c] = __builtin_fmaf(u, kf[c], st[c]);
+      for (int r = 0; r < 2; ++r) {
+        st[r][c] *= g;
+        d[r][c & 1] = __builtin_fmaf(st[r][c], kf[c], d[r][c & 1]);
+      }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) u[r] = now.beta * (bf16_to_f32(now.v[r]) - row_sum(d[r][0] + d[r][1]));
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) st[r][c] = __builtin_fmaf(u[r], kf[c], st[r][c]);
+    now = next;
   }
 #pragma unroll
-  for (int c = 0; c < NC; c += 4) *(f32x4*)(sp + c) = f32x4{st[c], st[c + 1], st[c + 2], st[c + 3]};
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < NC; c += 4)
+      *(f32x4*)(sp + r * kPairs * DK + c) = f32x4{st[r][c], st[r][c + 1], st[r][c + 2], st[r][c + 3]};
 }
 
 __device__ __forceinline__ void carry_rows(const AcceptArgs& a, int block) {
