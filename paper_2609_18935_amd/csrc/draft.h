@@ -13,6 +13,7 @@ struct DraftMasks {
   uint64_t m[kMaxDraft][2];
 };
 
+constexpr int kNormTokens = 4;   // tokens of a norm workgroup, at most
 struct NormArgs {
   const bf16_t* in[3];    // q, k, v (v is copied; draft_append only)
   bf16_t* out[3];
@@ -29,8 +30,9 @@ struct NormArgs {
   int32_t rotary;
   float eps;
   float weight_offset;
-  int32_t per_group;      // heads of one lane group
-  int32_t n_groups;       // lane groups of a token
+  int32_t tokens;         // of a workgroup
+  int32_t head_parts;     // workgroups that share the heads of a token
+  int32_t part_heads;     // heads of each of them
   int32_t use_depth;
   uint8_t depth[kMaxDraft];
 };

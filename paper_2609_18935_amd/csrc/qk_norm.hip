@@ -4,8 +4,9 @@
 // A row of one head is read once into registers, normed there, rotated and written: bound by
 // HBM for many tokens, by latency for one. D / 16 lanes hold a row, two chunks of 8 elements
 // a lane: in the rotated part the chunks j0 .. j0 + 7 and j0 + r/2 .. that form 8 pairs, so a
-// pair never leaves its lane, and behind it two chunks in a row. A lane forms the sines of its
-// 8 pairs once and goes through `per_group` heads of one token with them.
+// pair never leaves its lane, and behind it two chunks in a row. A workgroup forms the sines of
+// its few tokens once, into LDS, while its first rows are on their way, and shares them among
+// the tokens' heads.
 //
 // Angles: position * theta^(-2j/r) / (2 pi) is formed in float64 (turns; the rate of pair
 // 8 l + e is the product of two factors that come with the launch) and reduced to
@@ -61,34 +62,59 @@ template <int D, bool PAIRED>
 __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
   constexpr int LANES = D / 16;
   constexpr int kGroups = kThreads / LANES;
+  __shared__ __attribute__((aligned(16))) float s_cos[kNormTokens * D / 2];
+  __shared__ __attribute__((aligned(16))) float s_sin[kNormTokens * D / 2];
   __shared__ float s_row[PAIRED ? 1 : kGroups][PAIRED ? 1 : D];
-  const int group = blockIdx.x * kGroups + threadIdx.x / LANES;
-  const int l = threadIdx.x % LANES;
-  const int t = group / a.n_groups;
-  if (t >= a.T) return;
-  const int h0 = (group - t * a.n_groups) * a.per_group;
-  const int h1 = min(h0 + a.per_group, (int)a.heads_end[2]);
+  const int part = blockIdx.x % a.head_parts;
+  const int tok0 = blockIdx.x / a.head_parts * a.tokens, n_tok = min(a.tokens, a.T - tok0);
+  const int h0 = part * a.part_heads, nh = min(a.part_heads, a.heads_end[2] - h0);
+  const int g = threadIdx.x / LANES, l = threadIdx.x % LANES;
   const int r = a.rotary, half = r >> 1;
   const int turning = PAIRED ? half >> 3 : 0;   // lanes that hold pairs
   const bool turns = l < turning;
   const int ea = turns ? 8 * l : (PAIRED ? r : 0) + 16 * (l - turning);   // first elements of the two chunks
   const int eb = turns ? half + 8 * l : ea + 8;
 
-  double p = (double)(a.first_pos + (a.use_depth ? (int)a.depth[t] : t));
-  if (a.pos) p = (double)a.pos[t];
-  float sn[8], cs[8];
-  if (PAIRED && turns) {
-    const double rate = a.turn_lane[l] * p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) turn_sincos(rate * a.turn_elem[e], sn[e], cs[e]);
-  }
+  // rows (token, head) of the workgroup, head fastest, dealt out to the lane groups; read one
+  // ahead (in place too: a row is written by the lanes that have read it)
+  struct Row {
+    u32x4 a, b;
+  };
+  auto row_of = [&](int h, int& which, int& head) __attribute__((always_inline)) {
+    which = h < a.heads_end[0] ? 0 : h < a.heads_end[1] ? 1 : 2;
+    head = h - (which == 0 ? 0 : a.heads_end[which - 1]);
+  };
+  auto read = [&](int tok, int h) __attribute__((always_inline)) -> Row {
+    int which, head;
+    row_of(h0 + h, which, head);
+    const bf16_t* x = a.in[which] + (long)(tok0 + tok) * a.in_stride[which] + (long)head * D;
+    return Row{*(const u32x4*)(x + ea), *(const u32x4*)(x + eb)};
+  };
+  auto forward = [&](int& tok, int& h) __attribute__((always_inline)) {
+    for (h += kGroups; h >= nh && tok < n_tok; h -= nh) ++tok;
+  };
+  int tok = 0, h = g;
+  for (; h >= nh && tok < n_tok; h -= nh) ++tok;
+  Row next{};
+  if (tok < n_tok) next = read(tok, h);
 
-  for (int h = h0; h < h1; ++h) {
-    const int which = h < a.heads_end[0] ? 0 : h < a.heads_end[1] ? 1 : 2;
-    const int head = h - (which == 0 ? 0 : a.heads_end[which - 1]);
-    const bf16_t* x = a.in[which] + t * a.in_stride[which] + (long)head * D;
-    bf16_t* y = a.out[which] + t * a.out_stride[which] + (long)head * D;
-    const u32x4 wa = *(const u32x4*)(x + ea), wb = *(const u32x4*)(x + eb);
+  for (int i = threadIdx.x; i < n_tok * half; i += kThreads) {
+    const int t = i / half, j = i - t * half;
+    double p = (double)(a.first_pos + (a.use_depth ? (int)a.depth[tok0 + t] : tok0 + t));
+    if (a.pos) p = (double)a.pos[tok0 + t];
+    turn_sincos(p * (a.turn_lane[j >> 3] * a.turn_elem[j & 7]), s_sin[i], s_cos[i]);
+  }
+  __syncthreads();
+
+  while (tok < n_tok) {
+    int which, head;
+    row_of(h0 + h, which, head);
+    bf16_t* y = a.out[which] + (long)(tok0 + tok) * a.out_stride[which] + (long)head * D;
+    const float* cs = s_cos + tok * half;
+    const float* sn = s_sin + tok * half;
+    const u32x4 wa = next.a, wb = next.b;
+    forward(tok, h);
+    if (tok < n_tok) next = read(tok, h);
     if (which == 2) {   // values go as they are
       *(u32x4*)(y + ea) = wa;
       *(u32x4*)(y + eb) = wb;
@@ -103,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
       for (int e = 0; e < 16; ++e) ss = __builtin_fmaf(f[e], f[e], ss);
       ss = group_sum<LANES>(ss);
       if (a.kind == TU_NORM_RMS) ss *= 1.f / D;
-      const float inv = 1.f / sqrtf(ss + a.eps);
+      const float inv = __builtin_amdgcn_rsqf(ss + a.eps);   // within a step of fp32
 #pragma unroll
       for (int e = 0; e < 16; ++e) f[e] *= inv;
       if (a.kind == TU_NORM_RMS && a.weight[which]) {
@@ -116,16 +142,22 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
     }
     if constexpr (PAIRED) {
       if (turns) {
+        float c[8], s[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          *(f32x4*)(c + e) = *(const f32x4*)(cs + 8 * l + e);
+          *(f32x4*)(s + e) = *(const f32x4*)(sn + 8 * l + e);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float u = f[e], v = f[e + 8];
-          f[e] = u * cs[e] - v * sn[e];
-          f[e + 8] = v * cs[e] + u * sn[e];
+          f[e] = u * c[e] - v * s[e];
+          f[e + 8] = v * c[e] + u * s[e];
         }
       }
     } else {
       // a group lies in one wave, whose LDS accesses keep their order
-      float* row = s_row[threadIdx.x / LANES];
+      float* row = s_row[g];
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int e = 0; e < 16; ++e) row[ea + e] = f[e];
@@ -136,9 +168,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
         const int d = ea + e;
         if (d < r) {
           const int j = d < half ? d : d - half;
-          float s1, c1;
-          turn_sincos(a.turn_lane[j >> 3] * p * a.turn_elem[j & 7], s1, c1);
-          f[e] = d < half ? row[j] * c1 - row[j + half] * s1 : row[j + half] * c1 + row[j] * s1;
+          f[e] = d < half ? row[j] * cs[j] - row[j + half] * sn[j] : row[j + half] * cs[j] + row[j] * sn[j];
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -152,10 +182,9 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
 }  // namespace
 
 hipError_t launch_qk_norm(const NormArgs& a, int head_dim, hipStream_t s) {
-  const long groups = (long)a.T * a.n_groups;
-  if (groups <= 0) return hipSuccess;
-  const int per_block = kThreads * 16 / head_dim;
-  const long blocks = (groups + per_block - 1) / per_block;
+  if (a.T <= 0) return hipSuccess;
+  if (a.tokens < 1 || a.tokens > kNormTokens || a.part_heads * a.head_parts < a.heads_end[2]) return hipErrorInvalidValue;
+  const long blocks = (long)((a.T + a.tokens - 1) / a.tokens) * a.head_parts;
   const bool paired = (a.rotary & 15) == 0;
   const auto run = [&](auto pairs, auto any) {
     if (paired) hipLaunchKernelGGL(pairs, dim3(blocks), dim3(kThreads), 0, s, a);
