@@ -42,14 +42,9 @@ int check_norm(const tu_qk_norm* m) {
   return TU_OK;
 }
 
-// Depths of the nodes (0: a root); returns the largest.
-int draft_depths(const tu_draft* d, uint8_t* depth) {
-  int most = 0;
-  for (int i = 0; i < d->n; ++i) {
-    depth[i] = d->parent[i] < 0 ? 0 : (uint8_t)(depth[d->parent[i]] + 1);
-    most = std::max(most, (int)depth[i]);
-  }
-  return most;
+// Depths of the nodes (0: a root).
+void draft_depths(const tu_draft* d, uint8_t* depth) {
+  for (int i = 0; i < d->n; ++i) depth[i] = d->parent[i] < 0 ? 0 : (uint8_t)(depth[d->parent[i]] + 1);
 }
 
 void draft_masks(const tu_draft* d, DraftMasks* m) {
@@ -346,10 +341,6 @@ int draft_delta_rule(const float* state, const void* q, const void* k, const voi
     a.n_k_heads = p->n_k_heads;
     a.n_v_heads = p->n_v_heads;
     a.scale = p->scale;
-    uint8_t depth[kMaxDraft];
-    const int most = draft_depths(draft, depth);
-    while ((1 << a.rounds) <= most) ++a.rounds;
-    for (int i = 0; i < draft->n; ++i) a.parent[i] = (int16_t)draft->parent[i];
     draft_masks(draft, &a.seen);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (int e = hip_check(timed("draft_delta", st, [&] { return launch_draft_delta(a, p->d_k, st); }), "draft delta rule"))

@@ -85,9 +85,7 @@ struct DraftDeltaArgs {
   int32_t n;
   int32_t n_k_heads;
   int32_t n_v_heads;
-  int32_t rounds;       // pointer doublings that reach every root: 2^rounds > the deepest node's depth
   float scale;
-  int16_t parent[kMaxDraft];
   DraftMasks seen;
 };
 

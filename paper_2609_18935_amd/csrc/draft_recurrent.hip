@@ -118,9 +118,9 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   __shared__ __attribute__((aligned(16))) float s_a[tri(NB)][kBlock * kMStride];   // D o Q K^T
   __shared__ __attribute__((aligned(16))) float s_t[NB][kBlock * kMStride];        // (I + M_bb)^-1
   __shared__ __attribute__((aligned(16))) float s_rhs[kBlock][N + 4];              // [state row][node]
-  __shared__ double s_lg[2][kMaxDraft];     // log2 gamma
-  __shared__ int s_up[2][kMaxDraft];
-  __shared__ float s_beta[kMaxDraft];
+  __shared__ __attribute__((aligned(16))) bf16x8 s_k[NB][NK][64];   // K as the lanes of a product hold it
+  __shared__ double s_gate[N], lg[N];       // log2 of the gates; of gamma
+  __shared__ float s_beta[N];
   __shared__ unsigned long long s_bad[kBlock][2];   // nodes to leave out, for each state row
 
   const int Hv = a.n_v_heads, Hk = a.n_k_heads;
@@ -133,68 +133,107 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, col = lane & 15;
 
-  // gates: log2 gamma as float64 sums along the path, by pointer doubling
-  if (tid < N) {
-    const bool live = tid < n;
-    const float gin = live ? a.g[(long)tid * Hv + h] : 1.f;
-    const float gate = gin < 0x1p-100f ? 0x1p-100f : gin;   // as delta_rule_continue holds it
-    s_lg[0][tid] = (double)log2f(gate);
-    s_up[0][tid] = live ? a.parent[tid] : -1;
-    s_beta[tid] = live ? a.beta[(long)tid * Hv + h] : 0.f;
+  // ---- everything that comes from memory is asked for first: the gates (a thread a node), this
+  // wave's rows of K, Q and V, the workgroup's 16 rows of S, the masks
+  float gin = 1.f, bin = 0.f;
+  if (tid < n) {
+    gin = a.g[(long)tid * Hv + h];
+    bin = a.beta[(long)tid * Hv + h];
   }
-  if (tid < 2 * kBlock) s_bad[tid >> 1][tid & 1] = 0;
-
-  // this wave's rows of K and Q, and the workgroup's 16 rows of S in three terms
-  auto frag = [&](const bf16_t* base, int block, int s) __attribute__((always_inline)) -> bf16x8 {
-    const int node = min(block * kBlock + col, n - 1);
-    return __builtin_bit_cast(bf16x8, *(const u32x4*)(base + ((long)node * Hk + kh) * DK + 32 * s + 8 * g));
-  };
-  bf16x8 st[NK][3];
+  f32x4 sx[NK][2];
   {
     const float* sp = a.state + ((long)h * DK + i0 + col) * DK + 8 * g;
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
+      sx[s][0] = *(const f32x4*)(sp + 32 * s);
+      sx[s][1] = *(const f32x4*)(sp + 32 * s + 4);
+    }
+  }
+  bf16x8 kf[RB][NK], qf[RB][NK];
+  float vf[RB][4];
+  uint64_t see[RB][4][2];   // masks of this lane's nodes: rows 4 g + e of its blocks
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int b = rb ? NB - 1 - wave : wave;
+    if (b >= NB) continue;
+    const long at = ((long)min(b * kBlock + col, n - 1) * Hk + kh) * DK + 8 * g;   // rows past the last repeat it
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      kf[rb][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a.k + at + 32 * s));
+      qf[rb][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a.q + at + 32 * s));
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = b * kBlock + 4 * g + e;
+      vf[rb][e] = bf16_to_f32(a.v[((long)min(i, n - 1) * Hv + h) * DK + i0 + col]);
+      see[rb][e][0] = i < n ? a.seen.m[i][0] : 0;
+      see[rb][e][1] = i < n && NB > 4 ? a.seen.m[i][1] : 0;
+    }
+  }
+  // a thread's share of a node's path: PARTS neighbouring lanes a node
+  constexpr int PARTS = kThreads / N, SHARE = N / PARTS;
+  const int pnode = tid / PARTS, ppart = tid % PARTS;
+  uint64_t pmask = 0;
+  if (pnode < n) pmask = a.seen.m[pnode][ppart * SHARE >> 6] >> (ppart * SHARE & 63);
+
+  if (tid < N) {
+    const float gate = gin < 0x1p-100f ? 0x1p-100f : gin;   // as delta_rule_continue holds it
+    s_gate[tid] = (double)log2f(gate);
+    s_beta[tid] = bin;
+  }
+  if (tid < 2 * kBlock) s_bad[tid >> 1][tid & 1] = 0;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int b = rb ? NB - 1 - wave : wave;
+    if (b >= NB) continue;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) s_k[b][s][lane] = kf[rb][s];
+  }
+  __syncthreads();
+
+  // ---- log2 gamma: float64 sums of the gates along the paths
+  {
+    double x = 0.0;
+#pragma unroll 16
+    for (int j = 0; j < SHARE; ++j) {
+      const double y = s_gate[ppart * SHARE + j];
+      x += pmask >> j & 1 ? y : 0.0;
+    }
+#pragma unroll
+    for (int d = 1; d < PARTS; d <<= 1) x += __shfl_xor(x, d, 64);
+    if (ppart == 0) lg[pnode] = x;
+  }
+
+  // ---- products of this wave's rows with S, in three bf16 terms, the smallest first
+  f32x4 yk[RB], yq[RB];
+  {
+    bf16x8 st[NK][3];
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
       float x[8];
-      *(f32x4*)x = *(const f32x4*)(sp + 32 * s);
-      *(f32x4*)(x + 4) = *(const f32x4*)(sp + 32 * s + 4);
+      *(f32x4*)x = sx[s][0];
+      *(f32x4*)(x + 4) = sx[s][1];
       split3(x, st[s]);
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      yk[rb] = yq[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if ((rb ? NB - 1 - wave : wave) >= NB) continue;
+#pragma unroll
+      for (int p = 2; p >= 0; --p)
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+          yk[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[rb][s], st[s][p], yk[rb], 0, 0, 0);
+          yq[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[rb][s], st[s][p], yq[rb], 0, 0, 0);
+        }
     }
   }
   __syncthreads();
-  int cur = 0;
-  for (int r = 0; r < a.rounds; ++r) {
-    if (tid < N) {
-      const int up = s_up[cur][tid];
-      s_lg[cur ^ 1][tid] = s_lg[cur][tid] + (up >= 0 ? s_lg[cur][up] : 0.0);
-      s_up[cur ^ 1][tid] = up >= 0 ? s_up[cur][up] : -1;
-    }
-    __syncthreads();
-    cur ^= 1;
-  }
-  const double* lg = s_lg[cur];
 
-  f32x4 yq[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int b = rb ? NB - 1 - wave : wave;
     if (b >= NB || b * kBlock >= n) continue;
-    bf16x8 kf[NK], qf[NK];
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      kf[s] = frag(a.k, b, s);
-      qf[s] = frag(a.q, b, s);
-    }
-    f32x4 yk = {0.f, 0.f, 0.f, 0.f};
-    yq[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int p = 2; p >= 0; --p)
-#pragma unroll
-      for (int s = 0; s < NK; ++s) {
-        yk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s], st[s][p], yk, 0, 0, 0);
-        yq[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[s], st[s][p], yq[rb], 0, 0, 0);
-      }
-    // this lane's nodes: rows 4 g + e of block b
-    uint64_t see[4][2];
     double li[4];
     float bi[4];
     uint32_t bad = 0, bad_row = 0;   // bit e: node 4 g + e has an input that is not finite; for this state row
@@ -202,13 +241,10 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     for (int e = 0; e < 4; ++e) {
       const int i = b * kBlock + 4 * g + e;
       const bool live = i < n;
-      see[e][0] = live ? a.seen.m[i][0] : 0;
-      see[e][1] = live && NB > 4 ? a.seen.m[i][1] : 0;
       li[e] = lg[i];
       bi[e] = s_beta[i];
-      const float v = live ? bf16_to_f32(a.v[((long)i * Hv + h) * DK + i0 + col]) : 0.f;
       const float gam = __builtin_amdgcn_exp2f((float)li[e]);
-      float rhs = bi[e] * (v - gam * yk[e]);
+      float rhs = bi[e] * (vf[rb][e] - gam * yk[rb][e]);
       if (!live) rhs = 0.f;
       if (!finite(rhs)) {
         bad_row |= 1u << e;
@@ -221,9 +257,9 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
       f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NK; ++s) {
-        const bf16x8 kc = frag(a.k, c, s);
-        kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s], kc, kk, 0, 0, 0);
-        qk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[s], kc, qk, 0, 0, 0);
+        const bf16x8 kc = s_k[c][s][lane];
+        kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[rb][s], kc, kk, 0, 0, 0);
+        qk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[rb][s], kc, qk, 0, 0, 0);
       }
       const int j = c * kBlock + col;
       const double lj = lg[j];
@@ -232,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = b * kBlock + 4 * g + e;
-        const bool sees = (see[e][j >> 6] >> (j & 63)) & 1;
+        const bool sees = (NB > 4 && j >= 64 ? see[rb][e][1] : see[rb][e][0]) >> (j & 63) & 1;
         const float ratio = __builtin_amdgcn_exp2f((float)(li[e] - lj));
         float m = -bi[e] * ratio * kk[e];
         if (!finite(m)) {
@@ -297,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     for (int e = 0; e < 4; ++e) {
       const int i = b * kBlock + 4 * g + e;
       if (i >= n) continue;
-      const bool spoilt = (a.seen.m[i][0] & bad0) | (a.seen.m[i][1] & bad1);
+      const bool spoilt = (see[rb][e][0] & bad0) | (see[rb][e][1] & bad1);
       a.out[((long)i * Hv + h) * DK + i0 + col] = spoilt ? __builtin_nanf("") : a.scale * o[e];
     }
   }
