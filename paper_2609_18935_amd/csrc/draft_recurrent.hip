@@ -106,6 +106,15 @@ __device__ __forceinline__ f32x4 mma16(f32x4 A, f32x4 B, f32x4 acc) {
   return acc;
 }
 
+// x + the value of the lane that CTRL pairs this one with
+template <int CTRL>
+__device__ __forceinline__ double add_dpp(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
+  return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 constexpr int tri(int b) { return b * (b + 1) / 2; }
 
 template <int DK, int NB>   // NB: blocks of 16 nodes
@@ -114,12 +123,19 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   constexpr int NSL = DK / kBlock;          // workgroups of a head
   constexpr int N = NB * kBlock;
   constexpr int RB = NB > 4 ? 2 : 1;        // row blocks of a wave
-  __shared__ __attribute__((aligned(16))) float s_m[tri(NB)][kBlock * kMStride];   // -M
+  // -M; before it is formed, the 16 rows of S in three bf16 terms as the lanes of a product hold them
+  constexpr size_t kMBytes = sizeof(float) * tri(NB) * kBlock * kMStride, kSBytes = sizeof(bf16x8) * NK * 3 * 64;
+  __shared__ __attribute__((aligned(16))) char s_ms[kMBytes > kSBytes ? kMBytes : kSBytes];
+  auto s_m = (float(*)[kBlock * kMStride])s_ms;
+  auto s_s = (bf16x8(*)[3][64])s_ms;
   __shared__ __attribute__((aligned(16))) float s_a[tri(NB)][kBlock * kMStride];   // D o Q K^T
   __shared__ __attribute__((aligned(16))) float s_t[NB][kBlock * kMStride];        // (I + M_bb)^-1
   __shared__ __attribute__((aligned(16))) float s_rhs[kBlock][N + 4];              // [state row][node]
   __shared__ __attribute__((aligned(16))) bf16x8 s_k[NB][NK][64];   // K as the lanes of a product hold it
-  __shared__ double s_gate[N], lg[N];       // log2 of the gates; of gamma
+  __shared__ __attribute__((aligned(16))) bf16x8 s_q[NB == 4 ? NK : 1][64];        // Q of the last of 4 blocks
+  __shared__ double s_gate[N];              // log2 of the gates
+  __shared__ float s_lg[N][2];              // log2 gamma, in two fp32 terms
+  __shared__ uint64_t s_see[N][2];          // masks
   __shared__ float s_beta[N];
   __shared__ unsigned long long s_bad[kBlock][2];   // nodes to leave out, for each state row
 
@@ -136,22 +152,21 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   // ---- everything that comes from memory is asked for first: the gates (a thread a node), this
   // wave's rows of K, Q and V, the workgroup's 16 rows of S, the masks
   float gin = 1.f, bin = 0.f;
+  uint64_t see0 = 0, see1 = 0;
   if (tid < n) {
+    see0 = a.seen.m[tid][0];
+    see1 = a.seen.m[tid][1];
     gin = a.g[(long)tid * Hv + h];
     bin = a.beta[(long)tid * Hv + h];
   }
-  f32x4 sx[NK][2];
-  {
-    const float* sp = a.state + ((long)h * DK + i0 + col) * DK + 8 * g;
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      sx[s][0] = *(const f32x4*)(sp + 32 * s);
-      sx[s][1] = *(const f32x4*)(sp + 32 * s + 4);
-    }
+  float sx[8];   // wave s takes dims 32 s .. of S
+  if (wave < NK) {
+    const float* sp = a.state + ((long)h * DK + i0 + col) * DK + 8 * g + 32 * wave;
+    *(f32x4*)sx = *(const f32x4*)sp;
+    *(f32x4*)(sx + 4) = *(const f32x4*)(sp + 4);
   }
   bf16x8 kf[RB][NK], qf[RB][NK];
   float vf[RB][4];
-  uint64_t see[RB][4][2];   // masks of this lane's nodes: rows 4 g + e of its blocks
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int b = rb ? NB - 1 - wave : wave;
@@ -166,8 +181,6 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     for (int e = 0; e < 4; ++e) {
       const int i = b * kBlock + 4 * g + e;
       vf[rb][e] = bf16_to_f32(a.v[((long)min(i, n - 1) * Hv + h) * DK + i0 + col]);
-      see[rb][e][0] = i < n ? a.seen.m[i][0] : 0;
-      see[rb][e][1] = i < n && NB > 4 ? a.seen.m[i][1] : 0;
     }
   }
   // a thread's share of a node's path: PARTS neighbouring lanes a node
@@ -180,6 +193,8 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     const float gate = gin < 0x1p-100f ? 0x1p-100f : gin;   // as delta_rule_continue holds it
     s_gate[tid] = (double)log2f(gate);
     s_beta[tid] = bin;
+    s_see[tid][0] = see0;
+    s_see[tid][1] = see1;
   }
   if (tid < 2 * kBlock) s_bad[tid >> 1][tid & 1] = 0;
 #pragma unroll
@@ -187,21 +202,39 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     const int b = rb ? NB - 1 - wave : wave;
     if (b >= NB) continue;
 #pragma unroll
-    for (int s = 0; s < NK; ++s) s_k[b][s][lane] = kf[rb][s];
+    for (int s = 0; s < NK; ++s) {
+      s_k[b][s][lane] = kf[rb][s];
+      if (NB == 4 && b == 3) s_q[s][lane] = qf[rb][s];
+    }
+  }
+  if (wave < NK) {
+    bf16x8 t[3];
+    split3(sx, t);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) s_s[wave][p][lane] = t[p];
   }
   __syncthreads();
 
   // ---- log2 gamma: float64 sums of the gates along the paths
   {
-    double x = 0.0;
+    double x[2] = {0.0, 0.0};
 #pragma unroll 16
     for (int j = 0; j < SHARE; ++j) {
       const double y = s_gate[ppart * SHARE + j];
-      x += pmask >> j & 1 ? y : 0.0;
+      x[j & 1] += pmask >> j & 1 ? y : 0.0;
     }
-#pragma unroll
-    for (int d = 1; d < PARTS; d <<= 1) x += __shfl_xor(x, d, 64);
-    if (ppart == 0) lg[pnode] = x;
+    double sum = x[0] + x[1];
+    if (PARTS >= 2) sum = add_dpp<0xB1>(sum);     // quad_perm 1,0,3,2
+    if (PARTS >= 4) sum = add_dpp<0x4E>(sum);     // quad_perm 2,3,0,1
+    if (PARTS >= 8) sum = add_dpp<0x141>(sum);    // row_half_mirror
+    if (PARTS >= 16) sum = add_dpp<0x140>(sum);   // row_mirror
+    if (ppart == 0) {
+      // differences of two such logs lose nothing: the high terms' is exact where it matters (near
+      // each other), the low terms' is added
+      const float hi = (float)sum;
+      s_lg[pnode][0] = hi;
+      s_lg[pnode][1] = fabsf(hi) < __builtin_inff() ? (float)(sum - (double)hi) : 0.f;
+    }
   }
 
   // ---- products of this wave's rows with S, in three bf16 terms, the smallest first
@@ -209,12 +242,9 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   {
     bf16x8 st[NK][3];
 #pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      float x[8];
-      *(f32x4*)x = sx[s][0];
-      *(f32x4*)(x + 4) = sx[s][1];
-      split3(x, st[s]);
-    }
+    for (int s = 0; s < NK; ++s)
+#pragma unroll
+      for (int p = 0; p < 3; ++p) st[s][p] = s_s[s][p][lane];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       yk[rb] = yq[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -230,63 +260,90 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   }
   __syncthreads();
 
+  // ---- blocks of M and of D o Q K^T. A row block's wave forms its blocks; of the last of four
+  // rows waves 0 and 1 take one each.
+  struct Rows {   // of this lane's nodes 4 g + e of a block
+    float lh[4], ll[4], beta[4];
+    uint64_t see[4][NB > 4 ? 2 : 1];
+  };
+  auto rows_of = [&](int b) __attribute__((always_inline)) -> Rows {
+    Rows r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = b * kBlock + 4 * g + e;
+      r.lh[e] = s_lg[i][0];
+      r.ll[e] = s_lg[i][1];
+      r.beta[e] = s_beta[i];
+      r.see[e][0] = s_see[i][0];
+      if constexpr (NB > 4) r.see[e][1] = s_see[i][1];
+    }
+    return r;
+  };
+  auto pair = [&](int b, int c, const Rows& r, const bf16x8 (&kb)[NK], const bf16x8 (&qb)[NK]) __attribute__((always_inline)) -> uint32_t {
+    uint32_t bad = 0;   // bit e: node 4 g + e has a key, beta or gate that is not finite (diagonal blocks)
+    f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const bf16x8 kc = s_k[c][s][lane];
+      kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[s], kc, kk, 0, 0, 0);
+      qk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qb[s], kc, qk, 0, 0, 0);
+    }
+    const int j = c * kBlock + col;
+    const float jh = s_lg[j][0], jl = s_lg[j][1];
+    float* mb = s_m[tri(b) + c] + 4 * g * kMStride + col;
+    float* ab = s_a[tri(b) + c] + 4 * g * kMStride + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint64_t see = NB > 4 && c >= 4 ? r.see[e][NB > 4 ? 1 : 0] : r.see[e][0];
+      const bool sees = (uint32_t)(see >> (16 * (c & 3))) >> col & 1, self = b == c && 4 * g + e == col;
+      const float ratio = __builtin_amdgcn_exp2f((r.lh[e] - jh) + (r.ll[e] - jl));
+      float m = -r.beta[e] * ratio * kk[e];
+      if (!finite(m)) {
+        if (self) bad |= 1u << e;
+        m = 0.f;
+      }
+      mb[e * kMStride] = sees && !self ? m : 0.f;
+      ab[e * kMStride] = sees ? ratio * qk[e] : 0.f;
+    }
+    return bad;
+  };
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int b = rb ? NB - 1 - wave : wave;
     if (b >= NB || b * kBlock >= n) continue;
-    double li[4];
-    float bi[4];
-    uint32_t bad = 0, bad_row = 0;   // bit e: node 4 g + e has an input that is not finite; for this state row
+    const Rows r = rows_of(b);
+    uint32_t bad = 0, bad_row = 0;   // bad_row: for this state row
+    f32x4 rhs;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int i = b * kBlock + 4 * g + e;
-      const bool live = i < n;
-      li[e] = lg[i];
-      bi[e] = s_beta[i];
-      const float gam = __builtin_amdgcn_exp2f((float)li[e]);
-      float rhs = bi[e] * (vf[rb][e] - gam * yk[rb][e]);
-      if (!live) rhs = 0.f;
-      if (!finite(rhs)) {
+      const float gam = __builtin_amdgcn_exp2f(r.lh[e] + r.ll[e]);
+      rhs[e] = r.beta[e] * (vf[rb][e] - gam * yk[rb][e]);
+      if (b * kBlock + 4 * g + e >= n) rhs[e] = 0.f;
+      if (!finite(rhs[e])) {
         bad_row |= 1u << e;
-        rhs = 0.f;
+        rhs[e] = 0.f;
       }
-      s_rhs[col][i] = rhs;
       yq[rb][e] *= gam;
     }
-    for (int c = 0; c <= b; ++c) {
-      f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < NK; ++s) {
-        const bf16x8 kc = s_k[c][s][lane];
-        kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[rb][s], kc, kk, 0, 0, 0);
-        qk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[rb][s], kc, qk, 0, 0, 0);
-      }
-      const int j = c * kBlock + col;
-      const double lj = lg[j];
-      float* mb = s_m[tri(b) + c];
-      float* ab = s_a[tri(b) + c];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = b * kBlock + 4 * g + e;
-        const bool sees = (NB > 4 && j >= 64 ? see[rb][e][1] : see[rb][e][0]) >> (j & 63) & 1;
-        const float ratio = __builtin_amdgcn_exp2f((float)(li[e] - lj));
-        float m = -bi[e] * ratio * kk[e];
-        if (!finite(m)) {
-          if (i == j) bad |= 1u << e;
-          m = 0.f;
-        }
-        mb[(4 * g + e) * kMStride + col] = sees && i != j ? m : 0.f;
-        ab[(4 * g + e) * kMStride + col] = sees ? ratio * qk[e] : 0.f;
-      }
-    }
+    *(f32x4*)&s_rhs[col][b * kBlock + 4 * g] = rhs;
+    for (int c = NB == 4 && b == 3 ? 2 : 0; c <= b; ++c) bad |= pair(b, c, r, kf[rb], qf[rb]);
     if (bad | bad_row) {
       for (int e = 0; e < 4; ++e) {
         const int i = b * kBlock + 4 * g + e;
         if (bad_row >> e & 1) atomicOr(&s_bad[col][i >> 6], 1ull << (i & 63));
         if (bad >> e & 1)
-          for (int r = 0; r < kBlock; ++r) atomicOr(&s_bad[r][i >> 6], 1ull << (i & 63));
+          for (int x = 0; x < kBlock; ++x) atomicOr(&s_bad[x][i >> 6], 1ull << (i & 63));
       }
     }
+  }
+  if (NB == 4 && wave < 2 && 3 * kBlock < n) {
+    bf16x8 kb[NK], qb[NK];
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      kb[s] = s_k[3 < NB ? 3 : 0][s][lane];
+      qb[s] = s_q[NB == 4 ? s : 0][lane];
+    }
+    pair(3, wave, rows_of(3 < NB ? 3 : 0), kb, qb);
   }
   __syncthreads();
 
@@ -297,14 +354,15 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     float t[kBlock];
 #pragma unroll
     for (int i = 0; i < kBlock; ++i) {
-      float x0 = i == col ? 1.f : 0.f, x1 = 0.f;
+      float x[4] = {i == col ? 1.f : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < i; ++j) {
-        const float m = mb[i * kMStride + j];
-        if (j & 1) x1 = __builtin_fmaf(m, t[j], x1);
-        else x0 = __builtin_fmaf(m, t[j], x0);
+      for (int j = 0; j < i; j += 4) {
+        const f32x4 m = *(const f32x4*)(mb + i * kMStride + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < i) x[e] = __builtin_fmaf(m[e], t[j + e], x[e]);
       }
-      t[i] = x0 + x1;
+      t[i] = (x[0] + x[1]) + (x[2] + x[3]);
       s_t[b][i * kMStride + col] = t[i];
     }
   }
@@ -333,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     for (int e = 0; e < 4; ++e) {
       const int i = b * kBlock + 4 * g + e;
       if (i >= n) continue;
-      const bool spoilt = (see[rb][e][0] & bad0) | (see[rb][e][1] & bad1);
+      const bool spoilt = (s_see[i][0] & bad0) | (s_see[i][1] & bad1);
       a.out[((long)i * Hv + h) * DK + i0 + col] = spoilt ? __builtin_nanf("") : a.scale * o[e];
     }
   }
