@@ -92,13 +92,13 @@ void norm_record(const tu_attn_params* p, const tu_qk_norm* norm, int64_t T, Nor
 int draft_splits(const tu_attn_params* p, int64_t n, int64_t len) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   const int64_t tiles = (n * G + kDraftRows - 1) / kDraftRows;
-  const int64_t units = (len + n + kDraftUnit - 1) / kDraftUnit;
+  const int64_t keys = draft_stage_keys(p->head_dim), stages = (len + n + keys - 1) / keys;
   int64_t want = p->kv_splits > 0 ? p->kv_splits : kCus / std::max<int64_t>(1, p->n_kv_heads * tiles);
   // a split's rows span less than 2^31 bytes (its loads' offsets are 32 bits wide), with the
-  // units loaded past its end
-  const int64_t unit_bytes = (int64_t)kDraftUnit * p->n_kv_heads * p->head_dim * 2;
-  want = std::max(want, (units * unit_bytes) / (INT32_MAX - 8 * unit_bytes) + 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, units, kMaxDraftSplits}));
+  // stages loaded past its end
+  const int64_t stage_bytes = keys * p->n_kv_heads * p->head_dim * 2;
+  want = std::max(want, (stages * stage_bytes) / (INT32_MAX - 8 * stage_bytes) + 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, stages, kMaxDraftSplits}));
 }
 
 size_t attention_ws(const tu_attn_params* p, int64_t n, int splits) {
@@ -255,9 +255,9 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     a.group = p->n_q_heads / p->n_kv_heads;
     a.n_tiles = (n * a.group + kDraftRows - 1) / kDraftRows;
     a.n_splits = splits;
-    const int units = (int)((seq->len + n + kDraftUnit - 1) / kDraftUnit);
-    a.split_units = units / splits;
-    a.more_units = units % splits;
+    const int keys = draft_stage_keys(p->head_dim), stages = (int)((seq->len + n + keys - 1) / keys);
+    a.split_stages = stages / splits;
+    a.more_stages = stages % splits;
     a.inv_tiles = 1.f / a.n_tiles;
     a.inv_splits = 1.f / splits;
     a.inv_group = 1.f / a.group;

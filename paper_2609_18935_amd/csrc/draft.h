@@ -52,8 +52,8 @@ struct DraftAttnArgs {
   int32_t n_tiles;        // ceil(n * G / kDraftRows)
   int32_t n_splits;
   int32_t group;          // query heads per KV head
-  int32_t split_units;    // units of 32 keys of a split; the first more_units splits have one more
-  int32_t more_units;
+  int32_t split_stages;   // stages of a split; the first more_stages splits have one more
+  int32_t more_stages;
   float inv_tiles;        // reciprocals
   float inv_splits;
   float inv_group;
@@ -63,7 +63,10 @@ struct DraftAttnArgs {
 };
 constexpr int kMaxDraftSplits = 128;
 constexpr int kDraftRows = 256;         // packed query rows of an attention workgroup
-constexpr int kDraftUnit = 32;          // keys of a unit
+constexpr int kDraftUnit = 32;          // keys of a unit of the products
+// Keys of a stage: 16 KB of K, 16 KB of V; half of that with head_dim 64, where longer stages leave
+// short contexts too few of them.
+constexpr int draft_stage_keys(int head_dim) { return head_dim == 256 ? 32 : 64; }
 
 struct DraftConvArgs {
   ConvJob job[kMaxConvJobs];   // state is only read

@@ -3,8 +3,8 @@
 //
 // The G query heads of a KV head are packed as rows (row = node * G + h mod G). A workgroup
 // takes 256 rows (8 waves of 32, two per SIMD) of one KV head and one split of the key range.
-// K and V come as they lie in the cache, in units of 32 keys, by LDS DMA into rings of four
-// units, two to three of them in flight: the cache is asked for far ahead whatever the number
+// K and V come as they lie in the cache, in stages of 16 KB each (32 keys of 256 dims), by LDS
+// DMA into rings of four, two to three of them in flight: the cache is asked for far ahead whatever the number
 // of rows, and waves without rows only load.
 //
 // S^T = K Q^T on v_mfma_f32_32x32x16_bf16, so that a lane holds 16 keys of one query and the
@@ -14,15 +14,15 @@
 // reads them. O^T += V^T P^T on the f16 MFMA, V transposed on its way by ds_read_b64_tr_b16.
 // Softmax sums, the running maximum (moved only when exceeded by 2^8) and O are fp32.
 //
-// The two waves of a SIMD take turns: while waves 0 - 3 run the matrix products of a unit (P V of the
-// unit before, then K Q^T), waves 4 - 7 run the softmax of theirs, and a barrier later the
+// The two waves of a SIMD take turns: while waves 0 - 3 run the matrix products of a stage (P V of
+// the stage before, then K Q^T), waves 4 - 7 run the softmax of theirs, and a barrier later the
 // other way round, so that the matrix core always has a wave to feed it.
 //
 // A row of D dims lies in LDS as D / 8 chunks of 16 bytes, permuted within the row so that the
 // rows read together fall into different banks: chunk c of K row r at c ^ (r mod 16), of V row
 // r at c ^ 2 (r mod 8); less where a row has fewer chunks. Outputs leave through LDS as well, in whole rows.
 //
-// The tree only matters to the units that reach past row len: there each lane shifts its
+// The tree only matters to the units of 32 keys that reach past row len: there each lane shifts its
 // node's mask to the unit and drops the keys whose bit is clear.
 #include "attention_tile.h"
 #include "draft.h"
@@ -82,12 +82,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   constexpr int RC = D / 8;                  // 16-byte chunks per row
   constexpr int KSWZ = RC < 16 ? RC - 1 : 15;
   constexpr int VSWZ = RC / 2 < 8 ? RC / 2 - 1 : 7;
-  constexpr int NC = kUnit * RC;             // chunks of a unit of K (or V)
-  constexpr bool kHalf = NC < kThreads;      // waves 0 - 3 load K, waves 4 - 7 load V (each loads both otherwise)
-  constexpr int NL = kHalf ? 1 : NC / kThreads;   // loads of a thread for a unit of K or V
-  constexpr int PER = kHalf ? 1 : 2 * NL;         // loads of a thread for a unit
-  static_assert(kHalf ? NC == kThreads / 2 : NC % kThreads == 0, "whole loads per thread");
-  constexpr int UB = kUnit * D * 2;          // bytes of a unit
+  constexpr int SK = draft_stage_keys(D);    // keys of a stage
+  constexpr int SUB = SK / kUnit;            // units of a stage
+  constexpr int UB = SK * D * 2;             // bytes of a stage of K (or V)
+  constexpr int NL = UB / 16 / kThreads;     // loads of a thread for one of them
+  constexpr int PER = 2 * NL;                // loads of a thread for a stage
+  static_assert(NL * 16 * kThreads == UB && SUB * kUnit == SK, "whole loads and units");
   __shared__ __attribute__((aligned(4 * UB))) char g_k[4 * UB];   // the rings (aligned: addresses in them are xored)
   __shared__ __attribute__((aligned(4 * UB))) char g_v[4 * UB];
   __shared__ uint64_t s_mask[kDraftRows][2];   // masks of the rows' nodes (workgroups that reach the tree)
@@ -106,51 +106,46 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hl = lane >> 5, col = lane & 31;
-  // units u0 .. u1 - 1: equal shares, the first `more_units` splits one more
-  const int u0 = split * a.split_units + min(split, a.more_units);
-  const int u1 = u0 + a.split_units + (split < a.more_units ? 1 : 0);
+  // stages u0 .. u1 - 1: equal shares, the first `more_stages` splits one more
+  const int u0 = split * a.split_stages + min(split, a.more_stages);
+  const int u1 = u0 + a.split_stages + (split < a.more_stages ? 1 : 0);
   const int rs = Hkv * D;   // elements of a cache row
 
-  // ---- a unit: LDS chunk i * 512 + tid is loaded by load i of the thread. The resources start
-  // at the split's first row and end with its last one that holds data: rows past it, and units
-  // past the split, are zeros. (A split's rows span less than 2^31 bytes.) A further load's
-  // row lies a multiple of 16 rows on: the same chunk.
+  // ---- a stage: LDS chunk i * 512 + tid is loaded by load i of the thread. The resources start
+  // at the split's first row and end with its last one that holds data: rows past it, and
+  // stages past the split, are zeros. (A split's rows span less than 2^31 bytes.) The second
+  // load's row lies a multiple of 16 rows on (of 8 with 8 chunks): the same chunk.
   constexpr int LR = kThreads / RC;
-  static_assert(kHalf || (LR % (KSWZ + 1) == 0 && LR % (VSWZ + 1) == 0), "the loads of a thread take the same chunk");
-  const int lwave = kHalf ? wave & 3 : wave;
-  const bool lv = kHalf && wave >= 4;
-  const long start = (long)u0 * kUnit * rs + (long)hkv * D;
-  const uint32_t bytes = (uint32_t)(min((u1 - u0) * kUnit, len + n - u0 * kUnit) * rs * 2 - (rs - D) * 2);
+  static_assert(LR % (KSWZ + 1) == 0 && LR % (VSWZ + 1) == 0, "the loads of a thread take the same chunk");
+  const long start = (long)u0 * SK * rs + (long)hkv * D;
+  const uint32_t bytes = (uint32_t)(min((u1 - u0) * SK, len + n - u0 * SK) * rs * 2 - (rs - D) * 2);
   const u32x4 kres = buffer_of(a.k_cache + start, bytes), vres = buffer_of(a.v_cache + start, bytes);
-  uint32_t koff, voff;   // of the next unit to load
+  uint32_t koff, voff;   // of the next stage to load
   {
-    const int ltid = kHalf ? tid & (kThreads / 2 - 1) : tid;
-    const int lrow = ltid / RC, lc = ltid % RC;
+    const int lrow = tid / RC, lc = tid % RC;
     koff = (uint32_t)(lrow * rs * 2 + (lc ^ (lrow & KSWZ)) * 16);
     voff = (uint32_t)(lrow * rs * 2 + (lc ^ (2 * (lrow & VSWZ))) * 16);
   }
-  const uint32_t unit_bytes = (uint32_t)(kUnit * rs * 2);
-  const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_void*)g_k + lwave * 1024;
-  const uint32_t lds_v = (uint32_t)(uintptr_t)(lds_void*)g_v + lwave * 1024;
+  const uint32_t stage_bytes = (uint32_t)(SK * rs * 2);
+  const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_void*)g_k + wave * 1024;
+  const uint32_t lds_v = (uint32_t)(uintptr_t)(lds_void*)g_v + wave * 1024;
   auto load_k = [&](int place) __attribute__((always_inline)) {
-    if (lv) return;
 #pragma unroll
     for (int i = 0; i < NL; ++i) dma_lds(lds_k + place * UB + i * kThreads * 16, koff, kres, i * LR * rs * 2);
-    koff += unit_bytes;
+    koff += stage_bytes;
   };
   auto load_v = [&](int place) __attribute__((always_inline)) {
-    if (kHalf && !lv) return;
 #pragma unroll
     for (int i = 0; i < NL; ++i) dma_lds(lds_v + place * UB + i * kThreads * 16, voff, vres, i * LR * rs * 2);
-    voff += unit_bytes;
+    voff += stage_bytes;
   };
 
-  // the first units are asked for before anything else; Q is waited for with the first of them
+  // the first stages are asked for before anything else; Q is waited for with the first of them
   load_k(0);
   const int rows_total = n * G;
   const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
   // Q's rows are read a line at a time (four parts of a row, 64 / LPR rows a load) and go
-  // through the wave's own LDS, in a ring place that is free until the first unit, into the
+  // through the wave's own LDS, in a ring place that is free until the first step, into the
   // operands: lane (query, half) holds 8 dims of each 16.
   constexpr int LPR = D / 32;          // 16-byte chunks of a quarter row
   constexpr int QL = LPR / 2;          // loads of a quarter
@@ -170,14 +165,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int i = 0; i < QL; ++i) w[b * QL + i] = *(const u32x4*)(from[i] + b * (D / 4));
-    if (u1 * kUnit > len) mask = a.seen.m[node][hl];
+    if (u1 * SK > len) mask = a.seen.m[node][hl];
   }
   load_v(0);
   load_k(1);
   load_v(1);
   load_k(2);
   if (busy) {
-    if (u1 * kUnit > len) s_mask[wave * 32 + col][hl] = mask;
+    if (u1 * SK > len) s_mask[wave * 32 + col][hl] = mask;
     char* const mine = (wave < 4 ? g_k : g_v) + 3 * UB + (wave & 3) * (UB / 4);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
@@ -222,13 +217,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     return x;
   };
 
-  // ---- this thread's loads up to V of the unit in `place` and K of the next have landed (two
-  // units of loads are newer); its chunks of that V to f16, in place
+  // ---- this thread's loads up to V of the stage in `place` and K of the next have landed (two
+  // stages of loads are newer); its chunks of that V to f16, in place
   auto to_f16 = [&](int place) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));
     asm volatile("" ::: "memory");
-    if (kHalf && !lv) return;
-    u32x4* const at = (u32x4*)(g_v + place * UB + (fresh(tid) & (kHalf ? kThreads / 2 - 1 : kThreads - 1)) * 16);
+    u32x4* const at = (u32x4*)(g_v + place * UB + (fresh(tid) & (kThreads - 1)) * 16);
     u32x4 w[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) w[i] = at[i * kThreads];
@@ -247,11 +241,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     asm volatile("" : "+v"(big));   // here, not behind the next products with the values kept until then
   };
 
-  f32x16 sacc;
-  f16x8 pf[2];
+  f32x16 sacc[SUB];
+  f16x8 pf[SUB][2];
 
-  // ---- the matrix products: O^T += V^T P^T of the unit in ring place BV, then S^T of the one in
-  // BK (in this order P is gone when the scores come). LDS reads run kAhead fragments ahead: an
+  // ---- the matrix products: O^T += V^T P^T of the stage in one ring place, then S^T of the one in
+  // another (in this order P is gone when the scores come). LDS reads run kAhead fragments ahead: an
   // MFMA takes 32 cycles, a read over 100; more would not fit the registers.
   constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = 3;
   auto sched_reads = [&](auto nc, auto per) __attribute__((always_inline)) {
@@ -269,53 +263,65 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // lane group g reads keys 4 (g >> 1) + 0 .. 3 (+ 16 k16, + 8) at dims 32 db + 16 (g & 1) .. ;
     // the blocks that share an address follow one another
 #pragma unroll
-    for (int lo = 0; lo < (NDB < 4 ? NDB : 4); ++lo)
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-      for (int k16 = 0; k16 < 2; ++k16)
+      for (int lo = 0; lo < (NDB < 4 ? NDB : 4); ++lo)
 #pragma unroll
-        for (int db = lo; db < NDB; db += 4) {
-          const uint32_t at = (vx ^ (64 * lo)) + (db >> 2) * 256 + 16 * k16 * D * 2;
-          const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
-          const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 8 * D * 2));
-          const u32x2 w0 = __builtin_bit_cast(u32x2, x0), w1 = __builtin_bit_cast(u32x2, x1);
-          const f16x8 va = __builtin_bit_cast(f16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pf[k16], o[db], 0, 0, 0);
-        }
-    sched_reads(IntC<2 * NDB>{}, IntC<2>{});
+        for (int k16 = 0; k16 < 2; ++k16)
+#pragma unroll
+          for (int db = lo; db < NDB; db += 4) {
+            const uint32_t at = (vx ^ (64 * lo)) + (db >> 2) * 256 + (kUnit * u + 16 * k16) * D * 2;
+            const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+            const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 8 * D * 2));
+            const u32x2 w0 = __builtin_bit_cast(u32x2, x0), w1 = __builtin_bit_cast(u32x2, x1);
+            const f16x8 va = __builtin_bit_cast(f16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va, pf[u][k16], o[db], 0, 0, 0);
+          }
+    sched_reads(IntC<2 * NDB * SUB>{}, IntC<2>{});
   };
   auto qk = [&](int place) __attribute__((always_inline)) {
     const uint32_t kx = kaddr + place * UB;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sacc[e] = 0.f;
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sacc[u][e] = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       const int s = NS == 16 ? (i >> 1) + 8 * (i & 1) : i;   // steps that share an address follow one another
-      const bf16x8 ka = __builtin_bit_cast(
-          bf16x8, *(const lds_u32x4*)(uintptr_t)((kx ^ (32 * s & 16 * KSWZ)) + (32 * s & ~(16 * KSWZ))));
-      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[s], sacc, 0, 0, 0);
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const bf16x8 ka = __builtin_bit_cast(
+            bf16x8, *(const lds_u32x4*)(uintptr_t)((kx ^ (32 * s & 16 * KSWZ)) + (32 * s & ~(16 * KSWZ)) + kUnit * u * D * 2));
+        sacc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[s], sacc[u], 0, 0, 0);
+      }
     }
-    sched_reads(IntC<NS>{}, IntC<1>{});
+    sched_reads(IntC<NS * SUB>{}, IntC<1>{});
   };
 
-  // ---- softmax of unit u: the mask, the maximum, P in f16 in the key order of the operand
-  auto softmax = [&](int u) __attribute__((always_inline)) {
-    const int d = u * kUnit - len;
-    if (d + kUnit - 1 >= 0) {   // reaches the tree (uniform)
-      // bit x of `keys`: this query sees key u * 32 + x
-      uint32_t keys;
-      const uint32_t t = fresh(tid), mr = (t & ~63u) / 2 + (t & 31u);
-      const uint64_t m0 = s_mask[mr][0], m1 = s_mask[mr][1];
-      if (d <= 0) keys = (uint32_t)(m0 << -d) | ((1u << -d) - 1u);
-      else if (d < 64) keys = (uint32_t)(m0 >> d | m1 << (64 - d));
-      else keys = d < 128 ? (uint32_t)(m1 >> (d - 64)) : 0u;
-      keys >>= (t & 32u) >> 3;
+  // ---- softmax of a stage: the masks, the maximum, P in f16 in the key order of the operand
+  auto softmax = [&](int stage) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (!(keys >> (8 * (e >> 2) + (e & 3)) & 1)) sacc[e] = -__builtin_inff();
+    for (int u = 0; u < SUB; ++u) {
+      const int d = stage * SK + u * kUnit - len;
+      if (d + kUnit - 1 >= 0) {   // the unit reaches the tree (uniform)
+        // bit x of `keys`: this query sees key x of the unit
+        uint32_t keys;
+        const uint32_t t = fresh(tid), mr = (t & ~63u) / 2 + (t & 31u);
+        const uint64_t m0 = s_mask[mr][0], m1 = s_mask[mr][1];
+        if (d <= 0) keys = (uint32_t)(m0 << -d) | ((1u << -d) - 1u);
+        else if (d < 64) keys = (uint32_t)(m0 >> d | m1 << (64 - d));
+        else keys = d < 128 ? (uint32_t)(m1 >> (d - 64)) : 0u;
+        keys >>= (t & 32u) >> 3;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(keys >> (8 * (e >> 2) + (e & 3)) & 1)) sacc[u][e] = -__builtin_inff();
+      }
     }
     float mx = -__builtin_inff();
 #pragma unroll
-    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sacc[e]);
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sacc[u][e]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx),
                                                      __builtin_bit_cast(uint32_t, mx), false, false);
     mx = fmaxf(__builtin_bit_cast(float, (uint32_t)sw[0]), __builtin_bit_cast(float, (uint32_t)sw[1])) * c2;
@@ -330,19 +336,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const float m_use = m_run == -__builtin_inff() ? 0.f : m_run;
     float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e], c2, -m_use));
-      ps[e & 3] += p;
-      pf[e >> 3][e & 7] = (_Float16)p;
-    }
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[u][e], c2, -m_use));
+        ps[e & 3] += p;
+        pf[u][e >> 3][e & 7] = (_Float16)p;
+      }
     l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
   };
 
-  // ---- half-steps, a barrier before each: in half-step 2 t waves 0 - 3 form the products of unit
-  // t while waves 4 - 7 run the softmax of unit t - 1, in 2 t + 1 the other way round. K of
-  // unit t - 1 and V of unit t - 2 are no longer read from 2 t on: their places take units t + 3
-  // and t + 2. V of unit t is turned to f16 in 2 t and 2 t + 1 and first read in 2 t + 2.
-  const int n_units = u1 - u0;
+  // ---- half-steps, a barrier before each: in half-step 2 t waves 0 - 3 form the products of stage
+  // t while waves 4 - 7 run the softmax of stage t - 1, in 2 t + 1 the other way round. K of
+  // stage t - 1 and V of stage t - 2 are no longer read from 2 t on: their places take stages t + 3
+  // and t + 2. V of stage t is turned to f16 in 2 t and 2 t + 1 and first read in 2 t + 2.
+  const int n_stages = u1 - u0;
   constexpr int UNR = 2;
   auto refill = [&](int t) __attribute__((always_inline)) {
     load_k((t + 3) & 3);
@@ -371,20 +379,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
   };
   auto run = [&](auto step) __attribute__((always_inline)) {
-    for (int t = 0; t < n_units; t += UNR) {
+    for (int t = 0; t < n_stages; t += UNR) {
 #pragma unroll
       for (int i = 0; i < UNR; ++i)
-        if (i == 0 || t + i < n_units) step(t + i);
+        if (i == 0 || t + i < n_stages) step(t + i);
     }
   };
-  __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));   // K of the first unit
+  __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));   // K of the first stage
   if (wave < 4) run(early);
   else run(later);
   __builtin_amdgcn_s_waitcnt(vm_wait(0));   // the loads past the split's end: no write into LDS may come later
   wg_barrier();
   if (busy) {
     if (wave >= 4) softmax(u1 - 1);
-    pv((n_units - 1) & 3);
+    pv((n_stages - 1) & 3);
   }
   if (big >= 65520.f) status_raise(a.status, kFaultRange);
   wg_barrier();   // the rings are written over below
