@@ -550,8 +550,10 @@ int draft_append(const tu_seq* seq, void* k_cache, void* v_cache, const tu_attn_
  *  q_hat: device bf16 [n][n_q_heads][head_dim], normed and rotated;
  *  out:   device bf16 [n][n_q_heads][head_dim], what the output projection reads (softmax
  *         and sums in fp32, one rounding to bf16 at the end).
- * Values are read as f16 (see the input range above; TU_FAULT_RANGE). p->kv_splits as in
- * tail_prefill_attention.
+ * Values are read as f16 (see the input range above; TU_FAULT_RANGE for finite magnitudes of
+ * 2^16 or more). A node's key or value that is not finite (or beyond f16) reaches only the nodes that see it. The
+ * result does not depend on rows behind the last node. p->kv_splits as in
+ * tail_prefill_attention (more where a split's rows would span 2 GB).
  */
 size_t draft_attention_workspace_size(const tu_attn_params* p, int32_t n, int64_t len);
 int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache, const tu_attn_params* p,
@@ -574,7 +576,9 @@ int draft_short_conv(const tu_draft* draft, const tu_conv_tensor* tensors, int32
  * beta_i (gamma_i / gamma_j) (k_i . k_j) u_j (gamma: product of the gates along the path)
  *   o_i = scale (gamma_i S q_i + sum over ancestors and i of (gamma_i / gamma_j) (q_i . k_j) u_j).
  * Tensors as in delta_rule_continue with T == n; everything is held in fp32 (or products of
- * three bf16 terms that carry as many bits). p->chunk is not used. Needs no workspace.
+ * three bf16 terms that carry as many bits). An input of a node that is not finite reaches only
+ * the node and its descendants. g = 0 is computed as 2^-100; p->chunk is not used. Needs no
+ * workspace.
  */
 int draft_delta_rule(const float* state, const void* q, const void* k, const void* v, const float* beta,
                      const float* g, const tu_delta_params* p, const tu_draft* draft, float* out, void* stream);

@@ -618,7 +618,7 @@ class QkNorm:
 
     def _of(self, head_dim: int, device: int):
         for w in (self.q_weight, self.k_weight):
-            if w is not None:
+            if w is not None and (w.numel() != head_dim or w.get_device() != device):
                 _need(w, "norm weight", torch.bfloat16, (head_dim,), device)
         return self._ref
 
@@ -649,9 +649,9 @@ def qk_norm_rope(params: tu_attn_params, q: Optional[torch.Tensor], k: Optional[
 def _check_caches(ctx: "Context", k_cache, v_cache, params, dev):
     """Addresses of the caches, which must hold every row of the context's capacity."""
     Hkv, D = params.n_kv_heads, params.head_dim
-    for c, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if c.dim() != 3 or c.shape[0] < ctx.c.capacity or c.shape[1] != Hkv or c.shape[2] != D:
-            raise ValueError(f"{what} must be [>= {ctx.capacity}][{Hkv}][{D}], is {tuple(c.shape)}")
+    ks, vs = k_cache.shape, v_cache.shape
+    if ks != vs or len(ks) != 3 or ks[0] < ctx.c.capacity or ks[1] != Hkv or ks[2] != D:
+        raise ValueError(f"k_cache and v_cache must be [>= {ctx.capacity}][{Hkv}][{D}], are {tuple(ks)}, {tuple(vs)}")
     return _need(k_cache, "k_cache", torch.bfloat16, None, dev), _need(v_cache, "v_cache", torch.bfloat16, None, dev)
 
 

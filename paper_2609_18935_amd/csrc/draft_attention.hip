@@ -92,6 +92,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ __attribute__((aligned(4 * UB))) char g_v[4 * UB];
   __shared__ uint64_t s_mask[kDraftRows][2];   // masks of the rows' nodes (workgroups that reach the tree)
   __shared__ int s_row[kDraftRows];            // output rows
+  __shared__ unsigned long long s_spoilt[D][2];   // nodes whose value is not finite in f16, by dim
+  __shared__ int s_spoils;
 
   const int item = xcd_remap(blockIdx.x, gridDim.x);
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads;
@@ -167,6 +169,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int i = 0; i < QL; ++i) w[b * QL + i] = *(const u32x4*)(from[i] + b * (D / 4));
     if (u1 * SK > len) mask = a.seen.m[node][hl];
   }
+  if (u1 * SK > len) {
+    for (int i = tid; i < 2 * D; i += kThreads) s_spoilt[i >> 1][i & 1] = 0;
+    if (tid == 0) s_spoils = 0;
+  }
   load_v(0);
   load_k(1);
   load_v(1);
@@ -219,7 +225,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   // ---- this thread's loads up to V of the stage in `place` and K of the next have landed (two
   // stages of loads are newer); its chunks of that V to f16, in place
-  auto to_f16 = [&](int place) __attribute__((always_inline)) {
+  // A value of a node that is not finite must not reach nodes that do not see it (0 x NaN in a
+  // product): it becomes 0, and the outputs that do see it are set to NaN at the end.
+  auto to_f16 = [&](int place, int stage) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(vm_wait(2 * PER));
     asm volatile("" ::: "memory");
     u32x4* const at = (u32x4*)(g_v + place * UB + (fresh(tid) & (kThreads - 1)) * 16);
@@ -237,6 +245,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         x[2 * e + 1] = (_Float16)hi;
       }
       at[i * kThreads] = __builtin_bit_cast(u32x4, x);
+      if ((stage + 1) * SK > len) {   // uniform
+        const u32x4 bits = __builtin_bit_cast(u32x4, x);
+        bool odd = false;   // an exponent of ones
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= (~bits[e] & 0x7C00u) == 0 | (~bits[e] & 0x7C000000u) == 0;
+        const uint32_t t = fresh(tid);
+        const int row = t / RC + i * LR, node = stage * SK + row - len;
+        if (odd && node >= 0 && node < n) {
+          const int dim = ((t % RC) ^ (2 * (row & VSWZ))) * 8;
+          uint16_t* const half = (uint16_t*)(at + i * kThreads);
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e)
+            if ((~half[e] & 0x7C00u) == 0) {
+              half[e] = 0;
+              atomicOr(&s_spoilt[dim + e][node >> 6], 1ull << (node & 63));
+              s_spoils = 1;
+            }
+        }
+      }
     }
     asm volatile("" : "+v"(big));   // here, not behind the next products with the values kept until then
   };
@@ -365,13 +392,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     wg_barrier();
     if (busy) softmax(u0 + t);
-    to_f16(t & 3);
+    to_f16(t & 3, u0 + t);
   };
   auto later = [&](int t) __attribute__((always_inline)) {   // waves 4 - 7
     wg_barrier();
     refill(t);
     if (busy && t > 0) softmax(u0 + t - 1);
-    to_f16(t & 3);
+    to_f16(t & 3, u0 + t);
     wg_barrier();
     if (busy) {
       if (t > 0) pv((t - 1) & 3);
@@ -428,6 +455,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   else rows_out(f16x4{});
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(kLgkmWait0);
+  if (u1 * SK > len && s_spoils) {   // lane (row, half): every other chunk of the row
+    const uint64_t m0 = s_mask[wave * 32 + col_e][0], m1 = s_mask[wave * 32 + col_e][1];
+#pragma unroll 1
+    for (int c = hl_e; c < RC; c += 2) {
+      uint32_t which = 0;
+      for (int e = 0; e < 8; ++e) which |= (uint32_t)(((s_spoilt[8 * c + e][0] & m0) | (s_spoilt[8 * c + e][1] & m1)) != 0) << e;
+      uint16_t* at = (uint16_t*)((wave < 4 ? g_k : g_v) + (wave & 3) * UB + col_e * D * 2 + ((c ^ (col_e & KSWZ)) * 16));
+      for (int e = 0; e < 8; ++e)
+        if (which >> e & 1) at[e] = whole ? 0x7FC0 : 0x7E00;   // NaN in bf16, in f16
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kLgkmWait0);
+  }
   // rows past the last (s_row is -1) lie past the resource: their stores are dropped
   const __amdgpu_buffer_rsrc_t out_res = __builtin_amdgcn_make_buffer_rsrc(
       whole ? (void*)a.out : (void*)(a.part_o + (long)split * n * Hq * D), 0, n * Hq * D * 2, kBufWord3);

@@ -150,6 +150,37 @@ def test_attention_ignores_rows_behind_the_draft_and_hidden_nodes():
     assert out[7].isnan().all()
 
 
+@pytest.mark.parametrize("hq,hkv,D,rows,splits", [(16, 2, 256, 50, 0), (8, 2, 128, 700, 0), (16, 4, 64, 90, 1)])
+def test_attention_keeps_a_nodes_non_finite_value_from_nodes_that_do_not_see_it(hq, hkv, D, rows, splits):
+    rng = np.random.default_rng(D)
+    parents = tree("tree", 70)
+    n = len(parents)
+    kv = bf16(rng, 2, rows + n + 3, hkv, D)
+    clean = kv.clone()
+    kv[1, rows + 3, 1, 7] = float("nan")
+    kv[1, rows + 66, 0, 0] = float("inf")
+    kv[1, rows + 40, 1, D - 1] = 3e38          # beyond f16: the same, and reported
+    out, _, _, ws = _attn(hq, hkv, D, rows, parents, kv=kv, splits=splits)
+    _, want, bound, _ = _attn(hq, hkv, D, rows, parents, kv=clean, splits=splits)
+    spoilt = np.zeros(want.shape, bool)
+    G = hq // hkv
+    for i in range(n):
+        line = O.line(parents, i)
+        spoilt[i, G:2 * G, 7] |= 3 in line
+        spoilt[i, :G, 0] |= 66 in line
+        spoilt[i, G:2 * G, D - 1] |= 40 in line
+    got = f64(out)
+    assert spoilt.any() and not np.isfinite(got[spoilt]).any()
+    assert worst(got[~spoilt], want[~spoilt], np.broadcast_to(bound, want.shape)[~spoilt]) <= 1
+    assert tu.workspace_faults(ws) == 4
+    # a cached row is seen by every node
+    kv = clean.clone()
+    kv[1, 5, 0, 2] = float("nan")
+    out, _, _, _ = _attn(hq, hkv, D, rows, parents, kv=kv, splits=splits)
+    got = f64(out)
+    assert np.isnan(got[:, :G, 2]).all() and np.isfinite(np.delete(got, 2, axis=2)).all() and np.isfinite(got[:, G:]).all()
+
+
 def test_attention_reports_values_beyond_f16():
     rng = np.random.default_rng(6)
     kv = bf16(rng, 2, 64, 2, 128)
