@@ -503,7 +503,8 @@ typedef struct tu_draft {
  *   TU_NORM_L2    y = x / sqrt(sum(x^2) + eps)
  * then the pairs (j, j + rotary_dim/2) of y turn by position * rope_theta^(-2j/rotary_dim),
  * the angle reduced in float64. Everything between the bf16 input and the bf16 output
- * (nearest even) is held in fp32 or float64.
+ * (nearest even) is held in fp32 or float64; the squares are summed in fp32, so a row whose sum
+ * of squares (+ eps) leaves fp32's normal range comes out as zeros, infinities or NaN.
  *  q_weight, k_weight: device bf16 [head_dim], shared by the heads; NULL stands for weights
  *  of 1 (without offset). Only TU_NORM_RMS reads them. weight_offset 1 serves weights stored
  *  as their difference from 1.
@@ -602,8 +603,9 @@ int draft_delta_rule(const float* state, const void* q, const void* k, const voi
  *  target, proposal: device fp32 [n] rows of `vocab` values, non-negative, row strides in
  *            elements (at least vocab); tokens: device int32 [n] (a token outside [0, vocab)
  *            is never accepted; tokens[0] is not read); u: device fp32 [n] in [0, 1).
- *  result:   device int32 [n + 2]: accepted nodes (at least 1), the next token, then the
- *            accepted path from node 0 on, filled up with -1.
+ *  result:   device int32 [n + 2]: accepted nodes (at least 1; 0 only where a wait expired,
+ *            TU_FAULT_WAIT), the next token, then the accepted path from node 0 on, filled up
+ *            with -1.
  */
 size_t draft_verify_workspace_size(int32_t n, int64_t vocab);
 int draft_verify(const tu_draft* draft, const int32_t* tokens, const float* target, int64_t target_stride,
@@ -621,8 +623,8 @@ int draft_verify(const tu_draft* draft, const int32_t* tokens, const float* targ
  *    become the last width - 1 of the carried rows followed by the path's rows of x.
  * Then len and next_pos grow by n_path and the live positions by [next_pos, next_pos +
  * n_path); vt_rows stays (the V^T copies take the new rows with the next refresh).
- * attn may be NULL without attention layers, delta without delta layers. n_path 0 changes
- * nothing. Needs no workspace.
+ * No buffer may appear twice. attn may be NULL without attention layers, delta without delta
+ * layers. n_path 0 changes nothing. Needs no workspace.
  */
 int draft_accept(tu_seq* seq, const tu_draft* draft, const int32_t* path, int32_t n_path, const tu_layer_io* layers,
                  int32_t n_layers, const tu_attn_params* attn, const tu_delta_params* delta, const tu_conv_tensor* conv,

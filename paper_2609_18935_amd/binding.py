@@ -638,8 +638,9 @@ def qk_norm_rope(params: tu_attn_params, q: Optional[torch.Tensor], k: Optional[
             args.append((None, 0, None, 0))
             continue
         shape = (T, heads, D)
-        args.append((_need(x, what, torch.bfloat16, shape, dev, True), x.stride(0),
-                     _need(y, what + "_out", torch.bfloat16, shape, dev, True), y.stride(0)))
+        one = heads * D   # a single token's stride means nothing
+        args.append((_need(x, what, torch.bfloat16, shape, dev, True), x.stride(0) if T > 1 else one,
+                     _need(y, what + "_out", torch.bfloat16, shape, dev, True), y.stride(0) if T > 1 else one))
     (qp, qs, qo, qos), (kp, ks, ko, kos) = args
     pos = None if positions is None else _need(positions, "positions", torch.int32, (T,), dev)
     _check(lib().qk_norm_rope(ctypes.byref(params), None if norm is None else norm._of(D, dev), qp, qs, kp, ks, T,
@@ -666,9 +667,9 @@ def draft_append(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, par
     bf = torch.bfloat16
     _check(lib().draft_append(ctypes.byref(ctx.c), kc, vc, ctypes.byref(params),
                               None if norm is None else norm._of(D, dev), draft._ref,
-                              _need(q, "q", bf, (n, params.n_q_heads, D), dev, True), q.stride(0) if n else 0,
-                              _need(k, "k", bf, kv, dev, True), k.stride(0) if n else 0,
-                              _need(v, "v", bf, kv, dev, True), v.stride(0) if n else 0,
+                              _need(q, "q", bf, (n, params.n_q_heads, D), dev, True), q.stride(0) if n > 1 else params.n_q_heads * D,
+                              _need(k, "k", bf, kv, dev, True), k.stride(0) if n > 1 else params.n_kv_heads * D,
+                              _need(v, "v", bf, kv, dev, True), v.stride(0) if n > 1 else params.n_kv_heads * D,
                               _need(q_hat, "q_hat", bf, (n, params.n_q_heads, D), dev), _stream_on(stream, dev)))
 
 
@@ -781,6 +782,8 @@ class DraftStack:
         self.n_layers = len(layers)
         for L, c in zip(layers, self._layers):
             c.kind = L.kind
+            if len((L.k_cache if L.kind == TU_LAYER_ATTN else L.state) or ()) != 1:
+                raise ValueError("a draft continues one context: one cache or state a layer")
             if L.kind == TU_LAYER_ATTN:
                 if attn is None:
                     raise ValueError("attention layers need attn")

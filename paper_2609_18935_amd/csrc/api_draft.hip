@@ -107,6 +107,19 @@ size_t attention_ws(const tu_attn_params* p, int64_t n, int splits) {
   return kStatusBytes + align_up(rows * p->head_dim * sizeof(_Float16)) + align_up(rows * 2 * sizeof(float));
 }
 
+// The delta kernels' grids and offsets are 32 bits wide.
+int check_delta_heads(const tu_delta_params* p) {
+  if (int e = check_delta(p)) return e;
+  if (p->n_v_heads > UINT16_MAX) return fail(TU_ERR_ARG, "too many heads");
+  return TU_OK;
+}
+
+int check_channels(const char* what, int i, int32_t channels) {
+  if (channels <= 0 || channels % 8) return fail(TU_ERR_ARG, "%s %d: channels must be a positive multiple of 8", what, i);
+  if ((int64_t)channels * TU_MAX_DRAFT > INT32_MAX) return fail(TU_ERR_ARG, "%s %d: too many channels", what, i);
+  return TU_OK;
+}
+
 constexpr size_t kVerifyBytes = kStatusBytes + (kMaxDraft + 1) * kDrawMaxBlocks * sizeof(double);
 
 int check_workspace(const void* ws, size_t bytes, size_t need) {
@@ -230,6 +243,7 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
       return fail(TU_ERR_CAPACITY, "%lld rows + %d drafted exceed capacity %lld", (long long)seq->len, n,
                   (long long)seq->capacity);
     if (seq->len > INT32_MAX / 2) return fail(TU_ERR_ARG, "context too long");
+    if ((int64_t)n * p->n_q_heads * p->head_dim * 2 > INT32_MAX) return fail(TU_ERR_ARG, "too many heads");   // out, in bytes
     if (n == 0) return ok();
     if (!k_cache || !v_cache || !q_hat || !out) return fail(TU_ERR_ARG, "null tensor");
     if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q_hat) || !aligned16(out))
@@ -261,7 +275,7 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     a.inv_tiles = 1.f / a.n_tiles;
     a.inv_splits = 1.f / splits;
     a.inv_group = 1.f / a.group;
-    if ((int64_t)p->n_kv_heads * splits * a.n_tiles >= 1 << 21 || n * a.group >= 1 << 21)
+    if ((int64_t)p->n_kv_heads * splits * a.n_tiles >= 1 << 21 || n * a.group >= 1 << 21)   // quotient() in the kernel
       return fail(TU_ERR_ARG, "too many heads");
     a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
     draft_masks(draft, &a.seen);
@@ -285,8 +299,7 @@ int draft_short_conv(const tu_draft* draft, const tu_conv_tensor* tensors, int32
     for (int i = 0; i < n; ++i) {
       const tu_conv_tensor& t = tensors[i];
       if (t.T != draft->n) return fail(TU_ERR_ARG, "tensor %d has %lld rows, the draft %d nodes", i, (long long)t.T, draft->n);
-      if (t.channels <= 0 || t.channels % 8) return fail(TU_ERR_ARG, "tensor %d: channels must be a positive multiple of 8", i);
-      if ((int64_t)t.channels * TU_MAX_DRAFT > INT32_MAX) return fail(TU_ERR_ARG, "tensor %d: too many channels", i);
+      if (int e = check_channels("tensor", i, t.channels)) return e;
       if (draft->n == 0) continue;
       if (!t.x || !t.weight || !t.out || (!t.state && width > 1)) return fail(TU_ERR_ARG, "tensor %d: null pointer", i);
       if (!aligned16(t.x) || !aligned16(t.weight) || !aligned16(t.out) || (t.state && !aligned16(t.state)))
@@ -323,7 +336,7 @@ int draft_short_conv(const tu_draft* draft, const tu_conv_tensor* tensors, int32
 int draft_delta_rule(const float* state, const void* q, const void* k, const void* v, const float* beta,
                      const float* g, const tu_delta_params* p, const tu_draft* draft, float* out, void* stream) {
   return guarded([&]() -> int {
-    if (int e = check_delta(p)) return e;
+    if (int e = check_delta_heads(p)) return e;
     if (int e = check_draft(draft)) return e;
     if (draft->n == 0) return ok();
     if (!state || !q || !k || !v || !beta || !g || !out) return fail(TU_ERR_ARG, "null tensor");
@@ -445,11 +458,11 @@ int draft_accept(tu_seq* seq, const tu_draft* draft, const int32_t* path, int32_
     if (n_attn)
       if (int e = check_attn(attn)) return e;
     if (n_delta)
-      if (int e = check_delta(delta)) return e;
+      if (int e = check_delta_heads(delta)) return e;
     for (int i = 0; i < n_conv; ++i) {
       const tu_conv_tensor& t = conv[i];
       if (t.T != draft->n) return fail(TU_ERR_ARG, "convolution %d has %lld rows, the draft %d nodes", i, (long long)t.T, (int)draft->n);
-      if (t.channels <= 0 || t.channels % 8) return fail(TU_ERR_ARG, "convolution %d: channels must be a positive multiple of 8", i);
+      if (int e = check_channels("convolution", i, t.channels)) return e;
       if (width > 1 && (!t.state || !t.x)) return fail(TU_ERR_ARG, "convolution %d: null pointer", i);
       if (width > 1 && (!aligned16(t.state) || !aligned16(t.x))) return fail(TU_ERR_ARG, "convolution %d: not 16-byte aligned", i);
     }

@@ -172,3 +172,36 @@ def test_conv_widths_and_channels():
     _raises(B.TU_ERR_ARG, lambda: tu.draft_short_conv(d, [(None, z(2, 8), z(8, 2), z(2, 8))]))
     with pytest.raises(ValueError):
         tu.draft_short_conv(d, [(z(1, 8), z(2, 8), z(8, 2), z(2, 8)), (z(2, 8), z(2, 8), z(8, 3), z(2, 8))])
+
+
+def test_head_and_channel_counts_beyond_the_launches_offsets():
+    """The counts alone are refused, before any address matters (no such tensor exists here)."""
+    one = z(64)
+    p = ctypes.byref
+    many = tu.attn_params(1 << 17, 1, 64)
+    d = tu.Draft([i - 1 for i in range(128)])
+    c = _ctx(10, 200)
+    ws = z(1 << 12, dtype=torch.uint8)
+    assert B.lib().draft_attention(p(c.c), one.data_ptr(), one.data_ptr(), p(many), d._ref, one.data_ptr(), one.data_ptr(),
+                                   ws.data_ptr(), 1 << 40, None) == B.TU_ERR_ARG
+    assert b"too many heads" in B.lib().tu_last_error()
+    wide = tu.delta_params(1, 1 << 16, 64, 64, 16)
+    f = z(64, dtype=f32)
+    assert B.lib().draft_delta_rule(f.data_ptr(), one.data_ptr(), one.data_ptr(), one.data_ptr(), f.data_ptr(), f.data_ptr(),
+                                    p(wide), d._ref, f.data_ptr(), None) == B.TU_ERR_ARG
+    assert b"too many heads" in B.lib().tu_last_error()
+    t = (B.tu_conv_tensor * 1)(B.tu_conv_tensor(one.data_ptr(), one.data_ptr(), one.data_ptr(), one.data_ptr(), 128, 1 << 24, 0))
+    assert B.lib().draft_short_conv(d._ref, t, 1, 4, 0, None) == B.TU_ERR_ARG
+    assert b"too many channels" in B.lib().tu_last_error()
+    path = (ctypes.c_int32 * 1)(0)
+    assert B.lib().draft_accept(p(c.c), d._ref, path, 1, None, 0, None, None, t, 1, 4, None) == B.TU_ERR_ARG
+    assert b"too many channels" in B.lib().tu_last_error() and c.len == 10
+
+
+def test_a_stack_holds_one_context():
+    pair = tu.LayerIO(tu.TU_LAYER_ATTN, None, None, None, None, k_cache=[z(20, 2, 64)] * 2, v_cache=[z(20, 2, 64)] * 2)
+    with pytest.raises(ValueError):
+        tu.DraftStack([pair], ATTN)
+    with pytest.raises(ValueError):
+        tu.DraftStack([tu.LayerIO(tu.TU_LAYER_DELTA, None, z(3, 2, 64), z(3, 4, 64), None, beta=z(3, 4, dtype=f32),
+                                  g=z(3, 4, dtype=f32))], None, DELTA)
