@@ -101,9 +101,12 @@ int draft_splits(const tu_attn_params* p, int64_t n, int64_t len) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, stages, kMaxDraftSplits}));
 }
 
+// Partial rows of a split: those of whole waves.
+int64_t wave_rows(const tu_attn_params* p, int64_t n) { return (n * (p->n_q_heads / p->n_kv_heads) + 31) / 32 * 32 * p->n_kv_heads; }
+
 size_t attention_ws(const tu_attn_params* p, int64_t n, int splits) {
   if (splits <= 1) return kStatusBytes;
-  const size_t rows = (size_t)splits * n * p->n_q_heads;
+  const size_t rows = (size_t)splits * wave_rows(p, n);
   return kStatusBytes + align_up(rows * p->head_dim * sizeof(_Float16)) + align_up(rows * 2 * sizeof(float));
 }
 
@@ -257,7 +260,7 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     a.out = static_cast<bf16_t*>(out);
     Arena ar(after_status(workspace));
     if (splits > 1) {
-      const size_t rows = (size_t)splits * n * p->n_q_heads;
+      const size_t rows = (size_t)splits * wave_rows(p, n);
       a.part_o = static_cast<_Float16*>(ar.take(rows * p->head_dim * sizeof(_Float16)));
       a.part_ml = static_cast<float*>(ar.take(rows * 2 * sizeof(float)));
     }
@@ -268,6 +271,7 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     a.n_kv_heads = p->n_kv_heads;
     a.group = p->n_q_heads / p->n_kv_heads;
     a.n_tiles = (n * a.group + kDraftRows - 1) / kDraftRows;
+    a.n_waves = (n * a.group + 31) / 32;
     a.n_splits = splits;
     const int keys = draft_stage_keys(p->head_dim), stages = (int)((seq->len + n + keys - 1) / keys);
     a.split_stages = stages / splits;

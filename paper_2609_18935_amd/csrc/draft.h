@@ -42,8 +42,9 @@ struct DraftAttnArgs {
   const bf16_t* k_cache;  // [>= len + n][Hkv][D]
   const bf16_t* v_cache;
   bf16_t* out;            // [n][Hq][D]
-  _Float16* part_o;       // [splits][n * Hq][D] normalised partial outputs (unused when n_splits == 1)
-  float* part_ml;         // [n * Hq][splits][2] reference max (log2 units), sum
+  // unused when n_splits == 1:
+  _Float16* part_o;       // [splits][Hkv][n_waves][D / 16][64][8] normalised partial outputs, as the lanes hold them
+  float* part_ml;         // [Hkv][n_waves * 32][splits][2] reference max (log2 units), sum
   CallStatus status;
   int32_t len;
   int32_t n;
@@ -58,7 +59,7 @@ struct DraftAttnArgs {
   float inv_splits;
   float inv_group;
   float scale_log2;       // softmax_scale * log2(e)
-  int32_t pad;
+  int32_t n_waves;        // ceil(n * G / 32): waves with rows
   DraftMasks seen;
 };
 constexpr int kMaxDraftSplits = 128;

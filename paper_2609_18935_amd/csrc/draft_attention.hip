@@ -433,44 +433,49 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;   // 0: no key of this split is seen; NaN goes on
   const bool whole = a.n_splits == 1;
   const int row = s_row[wave * 32 + col_e];
-  if (!whole && hl_e == 0 && row >= 0) {
-    float* ml = a.part_ml + ((long)row * a.n_splits + split) * 2;
-    ml[0] = l_tot == 0.f ? -__builtin_inff() : m_run == -__builtin_inff() ? 0.f : m_run;
-    ml[1] = l_tot;
+  if (u1 * SK > len && s_spoils) {
+    const uint64_t m0 = s_mask[wave * 32 + col_e][0], m1 = s_mask[wave * 32 + col_e][1];
+#pragma unroll
+    for (int c = 0; c < 4 * NDB; ++c) {
+      asm volatile("" ::: "memory");   // one chunk's masks at a time
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int dim = 8 * c + 4 * hl_e + e;
+        if ((s_spoilt[dim][0] & m0) | (s_spoilt[dim][1] & m1)) o[c >> 2][4 * (c & 3) + e] = __builtin_nanf("");
+      }
+    }
+  }
+  auto chunk = [&](int c) __attribute__((always_inline)) -> f32x4 {   // dims 8 c + 4 hl .. + 3
+    const int db = c >> 2, i = c & 3;
+    return f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]} * inv;
+  };
+  if (!whole) {   // a partial output as the lanes hold it
+    if (row < 0) return;
+    const long at = (long)(split * Hkv + hkv) * a.n_waves + tile * (kDraftRows / 32) + wave;
+    _Float16* to = a.part_o + at * 32 * D + lane_e * 8;
+#pragma unroll
+    for (int p = 0; p < 2 * NDB; ++p) {
+      const f16x4 x = __builtin_convertvector(chunk(2 * p), f16x4), y = __builtin_convertvector(chunk(2 * p + 1), f16x4);
+      *(f16x8*)(to + p * 512) = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    if (hl_e == 0) {
+      float* ml = a.part_ml + ((long)((hkv * a.n_waves + tile * (kDraftRows / 32) + wave) * 32 + col_e) * a.n_splits + split) * 2;
+      ml[0] = l_tot == 0.f ? -__builtin_inff() : m_run == -__builtin_inff() ? 0.f : m_run;
+      ml[1] = l_tot;
+    }
+    return;
   }
   // the wave's 32 rows through its own place of the rings, then 16 bytes a lane in whole rows
   const uint32_t mine = (uint32_t)(uintptr_t)(lds_void*)(wave < 4 ? g_k : g_v) + (wave & 3) * UB;
   const uint32_t wr = mine + col_e * D * 2 + hl_e * 8 + (col_e & KSWZ) * 16;
-  auto rows_out = [&](auto type) __attribute__((always_inline)) {
-    typedef decltype(type) vec4;
 #pragma unroll
-    for (int c = 0; c < 4 * NDB; ++c) {
-      const int db = c >> 2, i = c & 3;
-      const f32x4 x = f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]} * inv;
-      *(__attribute__((address_space(3))) vec4*)(uintptr_t)((wr ^ (16 * c & 16 * KSWZ)) + (16 * c & ~(16 * KSWZ))) =
-          __builtin_convertvector(x, vec4);
-    }
-  };
-  if (whole) rows_out(bf16x4{});
-  else rows_out(f16x4{});
+  for (int c = 0; c < 4 * NDB; ++c)
+    *(__attribute__((address_space(3))) bf16x4*)(uintptr_t)((wr ^ (16 * c & 16 * KSWZ)) + (16 * c & ~(16 * KSWZ))) =
+        __builtin_convertvector(chunk(c), bf16x4);
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(kLgkmWait0);
-  if (u1 * SK > len && s_spoils) {   // lane (row, half): every other chunk of the row
-    const uint64_t m0 = s_mask[wave * 32 + col_e][0], m1 = s_mask[wave * 32 + col_e][1];
-#pragma unroll 1
-    for (int c = hl_e; c < RC; c += 2) {
-      uint32_t which = 0;
-      for (int e = 0; e < 8; ++e) which |= (uint32_t)(((s_spoilt[8 * c + e][0] & m0) | (s_spoilt[8 * c + e][1] & m1)) != 0) << e;
-      uint16_t* at = (uint16_t*)((wave < 4 ? g_k : g_v) + (wave & 3) * UB + col_e * D * 2 + ((c ^ (col_e & KSWZ)) * 16));
-      for (int e = 0; e < 8; ++e)
-        if (which >> e & 1) at[e] = whole ? 0x7FC0 : 0x7E00;   // NaN in bf16, in f16
-    }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(kLgkmWait0);
-  }
   // rows past the last (s_row is -1) lie past the resource: their stores are dropped
-  const __amdgpu_buffer_rsrc_t out_res = __builtin_amdgcn_make_buffer_rsrc(
-      whole ? (void*)a.out : (void*)(a.part_o + (long)split * n * Hq * D), 0, n * Hq * D * 2, kBufWord3);
+  const __amdgpu_buffer_rsrc_t out_res = __builtin_amdgcn_make_buffer_rsrc(a.out, 0, n * Hq * D * 2, kBufWord3);
 #pragma unroll
   for (int i = 0; i < kUnit * RC / 64; ++i) {
     const int q = i * 64 + lane_e, rr = q / RC, c = q % RC;
@@ -479,69 +484,75 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 }
 
-// Joins the splits: a workgroup takes 64 dims of one (node, head) row, 16 lanes of 4 dims; its
-// 16 lane groups take the splits in turn and are added up through LDS in a fixed order. Every
-// lane requests all of its splits at once, before the weights are known: one trip to memory.
+// Joins the splits. The partial outputs lie as the lanes of k_draft_attn held them: for each split,
+// KV head and 32 packed rows D / 16 pieces of 1 KB, 16 bytes a lane (half, row): dims 16 p + 4 half + e, and 8
+// further on. A workgroup takes 8 rows of one piece: 16 lanes, whose 16 groups take the splits
+// in turn and are added up through LDS in a fixed order. Every lane requests all of its splits
+// at once, before the weights are known: one trip to memory.
 constexpr int kMergeThreads = 256;
-constexpr int kMergeDims = 64;
-constexpr int kMergeLanes = kMergeDims / 4;
-constexpr int kMergeGroups = kMergeThreads / kMergeLanes;
+constexpr int kMergeRows = 8;
+constexpr int kMergeGroups = kMergeThreads / 16;
 constexpr int kMergeEach = kMaxDraftSplits / kMergeGroups;   // splits of a lane group
-static_assert(kMaxDraftSplits == 128, "two splits per lane of a wave");
+static_assert(kMergeThreads / 32 == kMergeRows && kMaxDraftSplits == 4 * 32, "32 lanes form a row's weights");
 
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) {
-  __shared__ float s_w[kMaxDraftSplits];
-  __shared__ __attribute__((aligned(16))) float s_o[kMergeGroups][kMergeDims];
-  constexpr int SLICES = D / kMergeDims;
-  const int row = blockIdx.x / SLICES, d0 = (blockIdx.x % SLICES) * kMergeDims;
-  const long R = (long)a.n * a.n_q_heads;
-  const int tid = threadIdx.x, lane = tid & 63, g = tid / kMergeLanes, l = tid % kMergeLanes;
+  constexpr int PIECES = D / 16;
+  __shared__ float s_w[kMergeRows][kMaxDraftSplits + 1], s_l[kMergeRows];
+  __shared__ __attribute__((aligned(16))) float s_o[kMergeGroups][kMergeRows][20];
+  const int rows = a.n * a.group;
+  const int piece = blockIdx.x / 4 % PIECES, part = blockIdx.x / (4 * PIECES);   // the four parts of a piece are neighbours
+  const int hkv = part / a.n_waves, r0 = (part - hkv * a.n_waves) * 32 + blockIdx.x % 4 * kMergeRows;
+  if (r0 >= rows) return;
+  const int tid = threadIdx.x, g = tid >> 4, col = tid & 7, hl = tid >> 3 & 1;
   const int ns = a.n_splits;
-  const float* ml = a.part_ml + (long)row * ns * 2;
+
   typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
-  f32x2 x[2];
+  const int wr = tid >> 5, wl = tid & 31;   // forms weights of row r0 + wr
+  f32x2 x[4];
+  const f32x2* ml = (const f32x2*)a.part_ml + ((long)hkv * a.n_waves * 32 + r0 + wr) * ns;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) x[i] = lane + 64 * i < ns ? *(const f32x2*)(ml + 2 * (lane + 64 * i)) : f32x2{-__builtin_inff(), 0.f};
-  const _Float16* po = a.part_o + (long)row * D + d0 + 4 * l;
-  f16x4 v[kMergeEach];
+  for (int i = 0; i < 4; ++i)
+    x[i] = r0 + wr < rows && wl + 32 * i < ns ? ml[wl + 32 * i] : f32x2{-__builtin_inff(), 0.f};
+  const _Float16* po = a.part_o + ((long)hkv * a.n_waves + r0 / 32) * 32 * D + piece * 512 + (hl * 32 + r0 % 32 + col) * 8;
+  const long each = (long)a.n_kv_heads * a.n_waves * 32 * D;   // of a split
+  f16x8 v[kMergeEach];
 #pragma unroll
   for (int i = 0; i < kMergeEach; ++i) {
     const int s = g + kMergeGroups * i;
-    v[i] = s < ns ? *(const f16x4*)(po + (long)s * R * D) : f16x4{};
+    v[i] = s < ns && r0 + col < rows ? *(const f16x8*)(po + s * each) : f16x8{};
   }
-  // weights of the splits: every wave forms them alike, the first one stores them
-  float M = fmaxf(x[0][0], x[1][0]);
+  float M = fmaxf(fmaxf(x[0][0], x[1][0]), fmaxf(x[2][0], x[3][0]));
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
-  float w[2], L = 0.f;
+  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
+  float L = 0.f;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    w[i] = x[i][0] == -__builtin_inff() ? 0.f : x[i][1] * __builtin_amdgcn_exp2f(x[i][0] - M);
-    L += w[i];
+  for (int i = 0; i < 4; ++i) {
+    const float w = x[i][0] == -__builtin_inff() ? 0.f : x[i][1] * __builtin_amdgcn_exp2f(x[i][0] - M);
+    s_w[wr][wl + 32 * i] = w;   // 0 past the last split
+    L += w;
   }
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) L += __shfl_xor(L, d, 64);
-  if (tid < 64) {
-    s_w[lane] = w[0];
-    s_w[lane + 64] = w[1];
-  }
+  for (int d = 16; d > 0; d >>= 1) L += __shfl_xor(L, d, 64);
+  if (wl == 0) s_l[wr] = L;
   __syncthreads();
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float acc[8] = {};
 #pragma unroll
   for (int i = 0; i < kMergeEach; ++i) {
-    const float ws = s_w[g + kMergeGroups * i];   // 0 past the last split
+    const float ws = s_w[col][g + kMergeGroups * i];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(ws, (float)v[i][e], acc[e]);
+    for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(ws, (float)v[i][e], acc[e]);
   }
-  *(f32x4*)&s_o[g][4 * l] = acc;
+  *(f32x4*)&s_o[g][col][4 * hl] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+  *(f32x4*)&s_o[g][col][4 * hl + 8] = f32x4{acc[4], acc[5], acc[6], acc[7]};
   __syncthreads();
-  if (tid < kMergeDims) {
-    float sum = 0.f;
+  const int out = tid >> 4, r = r0 + out, d = tid & 15;   // row, dim of the piece
+  if (out >= kMergeRows || r >= rows) return;
+  float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMergeGroups; ++i) sum += s_o[i][tid];
-    ((__bf16*)a.out)[(long)row * D + d0 + tid] = (__bf16)(sum / L);
-  }
+  for (int i = 0; i < kMergeGroups; ++i) sum += s_o[i][out][d];
+  const int node = r / a.group;
+  ((__bf16*)a.out)[((long)node * a.n_q_heads + hkv * a.group + (r - node * a.group)) * D + 16 * piece + d] = (__bf16)(sum / s_l[out]);
 }
 
 }  // namespace
@@ -560,12 +571,12 @@ hipError_t launch_draft_attention(const DraftAttnArgs& a, int head_dim, hipStrea
 }
 
 hipError_t launch_draft_merge(const DraftAttnArgs& a, int head_dim, hipStream_t s) {
-  const int rows = a.n * a.n_q_heads;
-  if (rows <= 0) return hipSuccess;
+  const int parts = a.n_kv_heads * a.n_waves * 4;
+  if (parts <= 0) return hipSuccess;
   switch (head_dim) {
-    case 256: hipLaunchKernelGGL(k_draft_merge<256>, dim3(rows * 4), dim3(kMergeThreads), 0, s, a); break;
-    case 128: hipLaunchKernelGGL(k_draft_merge<128>, dim3(rows * 2), dim3(kMergeThreads), 0, s, a); break;
-    case 64: hipLaunchKernelGGL(k_draft_merge<64>, dim3(rows * 1), dim3(kMergeThreads), 0, s, a); break;
+    case 256: hipLaunchKernelGGL(k_draft_merge<256>, dim3(parts * 16), dim3(kMergeThreads), 0, s, a); break;
+    case 128: hipLaunchKernelGGL(k_draft_merge<128>, dim3(parts * 8), dim3(kMergeThreads), 0, s, a); break;
+    case 64: hipLaunchKernelGGL(k_draft_merge<64>, dim3(parts * 4), dim3(kMergeThreads), 0, s, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
