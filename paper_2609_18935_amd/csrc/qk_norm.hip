@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
     int which, head;
     row_of(h0 + h, which, head);
     const bf16_t* x = a.in[which] + (long)(tok0 + tok) * a.in_stride[which] + (long)head * D;
-    return Row{*(const u32x4*)(x + ea), *(const u32x4*)(x + eb)};
+    return Row{__builtin_nontemporal_load((const u32x4*)(x + ea)), __builtin_nontemporal_load((const u32x4*)(x + eb))};
   };
   auto forward = [&](int& tok, int& h) __attribute__((always_inline)) {
     for (h += kGroups; h >= nh && tok < n_tok; h -= nh) ++tok;
