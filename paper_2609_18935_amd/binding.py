@@ -548,23 +548,22 @@ _ACTIVATIONS = {"silu": TU_CONV_SILU, "none": TU_CONV_IDENTITY}
 def _need(t: torch.Tensor, what: str, dtype, shape, device: int, strided: bool = False) -> int:
     """The tensor's address, once it is what a kernel will take it for: dtype, shape (None: not checked), device
     of the call (-1: host, for the checks alone), contiguous (strided: tokens may lie apart)."""
-    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape):
+    if t.dtype is dtype and t.get_device() == device and (shape is None or t.shape == shape):
+        if t.is_contiguous():
+            return t.data_ptr()
+        if not strided:
+            raise ValueError(f"{what} must be contiguous")
+        inner = 1
+        for size, step in zip(t.shape[:0:-1], t.stride()[:0:-1]):
+            if step != inner and size != 1:
+                raise ValueError(f"the rows of {what} must be contiguous")
+            inner *= size
         return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype}, is {t.dtype}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, has {tuple(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{what} is on {t.device}, the call is for {'cuda:%d' % device if device >= 0 else 'cpu'}")
-    inner = 1
-    for d in range(t.dim() - 1, 0, -1):
-        if t.shape[d] != 1 and t.stride(d) != inner:
-            break
-        inner *= t.shape[d]
-    else:
-        if strided:
-            return t.data_ptr()
-    raise ValueError(f"the rows of {what} must be contiguous" if strided else f"{what} must be contiguous")
+    raise ValueError(f"{what} is on {t.device}, the call is for {'cuda:%d' % device if device >= 0 else 'cpu'}")
 
 
 def _call_device(t: torch.Tensor) -> int:
@@ -696,18 +695,15 @@ def draft_short_conv(draft: Draft, items, activation: str = "silu", stream=None)
     """items: sequence of (state [W-1][C], x [n][C], weight [C][W], out [n][C]) bf16 tensors sharing one width: the
     convolution along each node's path, the states only read."""
     arr = (tu_conv_tensor * max(1, len(items)))()
-    W, bf, dev = None, torch.bfloat16, -1
+    W, bf, n, dev = None, torch.bfloat16, draft.n, _call_device(items[0][1]) if items else -1
     for i, (st, x, w, out) in enumerate(items):
-        dev = _call_device(x)
-        C = int(x.shape[1])
-        if W is not None and w.shape[1] != W:
+        C, width = w.shape
+        if W is not None and width != W:
             raise ValueError("all tensors of a batch share one width")
-        W = int(w.shape[1])
-        rows = (draft.n, C)
-        t = arr[i]
-        t.state = None if st is None else _need(st, "state", bf, (W - 1, C), dev)
-        t.x, t.weight = _need(x, "x", bf, rows, dev), _need(w, "weight", bf, (C, W), dev)
-        t.out, t.T, t.channels = _need(out, "out", bf, rows, dev), draft.n, C
+        W = width
+        arr[i] = tu_conv_tensor(None if st is None else _need(st, "state", bf, (W - 1, C), dev),
+                                _need(x, "x", bf, (n, C), dev), _need(w, "weight", bf, (C, W), dev),
+                                _need(out, "out", bf, (n, C), dev), n, C, 0)
     _check(lib().draft_short_conv(draft._ref, arr, len(items), W or 1, _ACTIVATIONS[activation], _stream_on(stream, dev)))
 
 
