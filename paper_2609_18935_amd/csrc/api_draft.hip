@@ -88,12 +88,24 @@ void norm_record(const tu_attn_params* p, const tu_qk_norm* norm, int64_t T, Nor
   a->part_heads = (heads + a->head_parts - 1) / a->head_parts;
 }
 
-// Workgroups of the attention kernel over the key range: enough that every CU has one.
+// Workgroups of the attention kernel over the key range: at most one per CU, as they need all of its
+// LDS. A stage of a split takes about as long as 2.6 MB of partial outputs on their way through memory,
+// so stages * (splits' partial outputs) is least at the root below: 24 nodes of 16 + 2 heads of 256
+// over 3,000 rows 95 splits of one stage 21.8 us, 32 of three 17.3, 16 of six 19.9; one node 95 splits 10.4, 48 10.7.
+// Up to three stages more than a split's are no reason to split: the join costs a launch (64 nodes over
+// no rows, two stages: 11.2 us in one split, 15.3 in two; 24 nodes over 100 rows, four: 12.3 and 12.8; over
+// 200 rows, seven: 16.1 and 12.9).
 int draft_splits(const tu_attn_params* p, int64_t n, int64_t len) {
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   const int64_t tiles = (n * G + kDraftRows - 1) / kDraftRows;
   const int64_t keys = draft_stage_keys(p->head_dim), stages = (len + n + keys - 1) / keys;
-  int64_t want = p->kv_splits > 0 ? p->kv_splits : kCus / std::max<int64_t>(1, p->n_kv_heads * tiles);
+  int64_t want = p->kv_splits;
+  if (want == 0) {
+    const int64_t most = std::max<int64_t>(1, kCus / (p->n_kv_heads * std::max<int64_t>(1, tiles)));
+    const double partial = n * p->n_q_heads * p->head_dim * 2.0 / 2.6e6;   // of a split, in stages
+    const int64_t least = (stages + most - 1) / most, each = (int64_t)(std::sqrt(stages * partial) + 0.4);
+    want = stages <= std::max(least, each) + 3 ? 1 : each > least ? (stages + each - 1) / each : most;
+  }
   // a split's rows span less than 2^31 bytes (its loads' offsets are 32 bits wide), with the
   // stages loaded past its end
   const int64_t stage_bytes = keys * p->n_kv_heads * p->head_dim * 2;

@@ -205,3 +205,31 @@ def test_a_stack_holds_one_context():
     with pytest.raises(ValueError):
         tu.DraftStack([tu.LayerIO(tu.TU_LAYER_DELTA, None, z(3, 2, 64), z(3, 4, 64), None, beta=z(3, 4, dtype=f32),
                                   g=z(3, 4, dtype=f32))], None, DELTA)
+
+
+def _splits(p, rows, n):
+    """Splits of the key range, read off the workspace's size."""
+    size = B.lib().draft_attention_workspace_size(ctypes.byref(p), n, rows)
+    if size == 256:
+        return 1
+    waves = -(-n * (p.n_q_heads // p.n_kv_heads) // 32) * p.n_kv_heads
+    s = round((size - 256) / (waves * 32 * (p.head_dim * 2 + 8)))
+    up = lambda x: -(-x // 256) * 256
+    assert size == 256 + up(s * waves * 32 * p.head_dim * 2) + up(s * waves * 32 * 8)
+    return s
+
+
+def test_splits_of_the_attention():
+    big, mid = tu.attn_params(16, 2, 256), tu.attn_params(32, 8, 128)
+    for p in (big, mid):                                  # a few stages of 16 KB of keys are not split
+        assert [_splits(p, r, 24) for r in (0, 1, 40)] == [1, 1, 1]
+        assert _splits(p, 600, 1) > 4
+    assert _splits(big, 32767, 1) == 128 and _splits(big, 65536, 64) == 64     # a workgroup on every CU
+    assert _splits(big, 2976, 1) == 94 and _splits(big, 2976, 24) == 32        # partial outputs cost more with more rows
+    for n in (1, 7, 24, 64, 128):
+        for rows in (0, 1, 31, 500, 5000, 200000):
+            for p in (big, mid, tu.attn_params(40, 1, 64)):
+                assert 1 <= _splits(p, rows, n) <= 128
+    for s in (1, 2, 7, 64):                               # as asked for, as far as there are stages
+        assert _splits(tu.attn_params(16, 2, 256, kv_splits=s), 4096, 24) == s
+    assert _splits(tu.attn_params(16, 2, 256, kv_splits=64), 60, 4) == 2
