@@ -4,26 +4,35 @@
 // The G query heads of a KV head are packed as rows (row = node * G + h mod G). A workgroup
 // takes 256 rows (8 waves of 32, two per SIMD) of one KV head and one split of the key range.
 // K and V come as they lie in the cache, in stages of 16 KB each (32 keys of 256 dims), by LDS
-// DMA into rings of four, two to three of them in flight: the cache is asked for far ahead whatever the number
-// of rows, and waves without rows only load.
+// DMA into rings of four, two to three of them in flight: the cache is asked for far ahead whatever
+// the number of rows, and waves without rows only load.
 //
 // S^T = K Q^T on v_mfma_f32_32x32x16_bf16, so that a lane holds 16 keys of one query and the
 // running maximum and sum are per lane. P is rounded to f16 (10 stored mantissa bits; bf16's 7
 // would add an error as large as the output's own rounding), so V must be f16 too: every
 // thread turns the chunks that it has itself loaded into f16 in place, a barrier before anyone
 // reads them. O^T += V^T P^T on the f16 MFMA, V transposed on its way by ds_read_b64_tr_b16.
-// Softmax sums, the running maximum (moved only when exceeded by 2^8) and O are fp32.
+// Softmax sums, the running maximum (moved only when exceeded by 2^8) and O are fp32; partial
+// outputs of splits are normalised and rounded to f16.
 //
 // The two waves of a SIMD take turns: while waves 0 - 3 run the matrix products of a stage (P V of
 // the stage before, then K Q^T), waves 4 - 7 run the softmax of theirs, and a barrier later the
 // other way round, so that the matrix core always has a wave to feed it.
 //
 // A row of D dims lies in LDS as D / 8 chunks of 16 bytes, permuted within the row so that the
-// rows read together fall into different banks: chunk c of K row r at c ^ (r mod 16), of V row
-// r at c ^ 2 (r mod 8); less where a row has fewer chunks. Outputs leave through LDS as well, in whole rows.
+// rows read together fall into different banks: chunk c of K row r at c ^ (r mod 16), of V row r at
+// c ^ 4 (r mod 4) (four chunks of four rows at a time); less where a row has fewer chunks. With 2 (r mod 8)
+// for V, 29 % of the LDS's busy cycles were conflicts; now 1 %.
 //
 // The tree only matters to the units of 32 keys that reach past row len: there each lane shifts its
 // node's mask to the unit and drops the keys whose bit is clear.
+//
+// Measured with heads 16 / 2 of 256: 64 nodes over 65,536 rows 71 us (135 MB, 69 GFLOP) + 8 for the
+// join, about 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an 8192^3 bf16 matrix product sustains here;
+// the matrix cores are busy in 53 % of all cycles, 62 % within the loop): bound by the matrix cores at the clock
+// that the power allows. One node over 32,768 rows 15.5 us + 4: HBM (67 MB, 4.3 TB/s). 24
+// nodes over 11,907 rows 15.5 + 5: Q (96 KB a workgroup) and partial outputs (96 KB) cost as much as the
+// four stages between them. One node over 300 rows 9 us with the join: latency.
 #include "attention_tile.h"
 #include "draft.h"
 
@@ -83,7 +92,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   constexpr int NDB = D / 32;                // 32-dim blocks of O^T
   constexpr int RC = D / 8;                  // 16-byte chunks per row
   constexpr int KSWZ = RC < 16 ? RC - 1 : 15;
-  constexpr int VSWZ = RC / 2 < 8 ? RC / 2 - 1 : 7;
+  auto vswz = [](int row) __attribute__((always_inline)) { return RC < 16 ? (row & 2) * 2 : (row & 3) * 4; };
   constexpr int SK = draft_stage_keys(D);    // keys of a stage
   constexpr int SUB = SK / kUnit;            // units of a stage
   constexpr int UB = SK * D * 2;             // bytes of a stage of K (or V)
@@ -120,7 +129,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   // stages past the split, are zeros. (A split's rows span less than 2^31 bytes.) The second
   // load's row lies a multiple of 16 rows on (of 8 with 8 chunks): the same chunk.
   constexpr int LR = kThreads / RC;
-  static_assert(LR % (KSWZ + 1) == 0 && LR % (VSWZ + 1) == 0, "the loads of a thread take the same chunk");
+  static_assert(LR % (KSWZ + 1) == 0 && LR % 4 == 0, "the loads of a thread take the same chunk");
   const long start = (long)u0 * SK * rs + (long)hkv * D;
   const uint32_t bytes = (uint32_t)(min((u1 - u0) * SK, len + n - u0 * SK) * rs * 2 - (rs - D) * 2);
   const u32x4 kres = buffer_of(a.k_cache + start, bytes), vres = buffer_of(a.v_cache + start, bytes);
@@ -128,7 +137,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   {
     const int lrow = tid / RC, lc = tid % RC;
     koff = (uint32_t)(lrow * rs * 2 + (lc ^ (lrow & KSWZ)) * 16);
-    voff = (uint32_t)(lrow * rs * 2 + (lc ^ (2 * (lrow & VSWZ))) * 16);
+    voff = (uint32_t)(lrow * rs * 2 + (lc ^ vswz(lrow)) * 16);
   }
   const uint32_t stage_bytes = (uint32_t)(SK * rs * 2);
   const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_void*)g_k + wave * 1024;
@@ -214,7 +223,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int i = lane & 15, g = lane >> 4;
     const int row = 4 * (g >> 1) + (i >> 2);
     const int c0 = 2 * (g & 1) + ((i & 3) >> 1);
-    vaddr = (uint32_t)(uintptr_t)(lds_void*)g_v + (uint32_t)(row * D * 2 + ((c0 ^ (2 * (row & VSWZ))) * 16) + (i & 1) * 8);
+    vaddr = (uint32_t)(uintptr_t)(lds_void*)g_v + (uint32_t)(row * D * 2 + ((c0 ^ vswz(row)) * 16) + (i & 1) * 8);
   }
   // K row `col`, chunk hl ^ (col mod 16); chunk 2 s + hl is this address ^ 32 s
   const uint32_t kaddr = (uint32_t)(uintptr_t)(lds_void*)g_k + (uint32_t)(col * D * 2 + ((hl ^ (col & KSWZ)) * 16));
@@ -255,7 +264,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         const uint32_t t = fresh(tid);
         const int row = t / RC + i * LR, node = stage * SK + row - len;
         if (odd && node >= 0 && node < n) {
-          const int dim = ((t % RC) ^ (2 * (row & VSWZ))) * 8;
+          const int dim = ((t % RC) ^ vswz(row)) * 8;
           uint16_t* const half = (uint16_t*)(at + i * kThreads);
 #pragma unroll 1
           for (int e = 0; e < 8; ++e)
