@@ -78,9 +78,9 @@ void norm_record(const tu_attn_params* p, const tu_qk_norm* norm, int64_t T, Nor
   a->weight[0] = norm ? static_cast<const bf16_t*>(norm->q_weight) : nullptr;
   a->weight[1] = norm ? static_cast<const bf16_t*>(norm->k_weight) : nullptr;
   const int heads = a->heads_end[2];
-  // A workgroup takes 2 or 4 tokens where that leaves the chip full of them (eight per CU fit; 8,191
-  // tokens of 16 + 2 heads of 256: 1, 2, 3, 4 or 8 a workgroup 36.9, 36.4, 41.0, 36.2, 43.2 us); with few
-  // tokens their heads go to several, so that every lane group has a row.
+  // A workgroup takes 2 or 4 tokens where that leaves the chip full of them (eight per CU fit; 16 + 2
+  // heads of 256, 1, 2 or 4 a workgroup: 2,048 tokens 12.0, 12.7, 16.3 us; 4,096 21.2, 19.4, 23.1;
+  // 8,191 34.0, 32.2, 31.8); with few tokens their heads go to several, so that every lane group has a row.
   const int groups = 256 * 16 / p->head_dim;
   a->tokens = T > 3 * 8 * kCus ? 4 : T > 8 * kCus ? 2 : 1;
   const int most = (heads + groups - 1) / groups;

@@ -4,7 +4,10 @@
 // Delta states: the recurrence token by token along the path, as k_delta_step without outputs:
 // 16 lanes hold a row of one value head in registers from the first token to the last, two rows
 // at a time (two chains of dependent sums in flight, a token's operands read once for both).
-// Bound by HBM: each state is read and written once.
+// Bound by HBM: each state is read and written once. Measured: six tokens into 36 states of 32 heads
+// of 128 x 128, 12 pairs of caches and 36 convolutions of 8,192 channels 35 us in one launch (158 MB,
+// 4.5 TB/s; a copy 5.06); three tokens into three of each state and one pair of caches 5.4 us (latency: the
+// tokens one behind the other).
 //
 // Cache rows: a thread takes one 16-byte column of a K or V buffer and moves it row by row in
 // path order. Row len + j only ever overwrites rows whose own move came earlier (path[j] >= j,

@@ -4,7 +4,7 @@
 // Convolution. A thread takes 8 channels of one node: the rows under the taps are the node's
 // and those of its ancestors, then the carried ones; products are summed in fp32 in tap order
 // and rounded once to bf16. Bound by latency and issue: a layer's rows and weights (a few MB)
-// stay in L2.
+// stay in L2. Measured, 8,192 channels of width 4: one node 3.0 us, 64 3.7, 128 4.6.
 //
 // Delta rule. Evaluated token by token a tree needs a state (d x d fp32) per node; in the
 // WY form it needs the carried state once. With D_ij = gamma_i / gamma_j where j is an ancestor
@@ -18,12 +18,19 @@
 // triangular solve and the last product run on the fp32 MFMA. Nothing is rounded below fp32.
 //
 // Nodes go in blocks of 16. Wave w forms row block w (and the mirrored one of the upper half
-// when there are 8): its products with the blocks before it and with S. Then one lane per
+// when there are 8; of the last of four rows waves 0 and 1, which have little to do, take a block
+// each): its products with the blocks before it and with S, whose three terms one wave a
+// part has split for all. Then one lane per
 // column inverts the diagonal blocks I + M_bb by forward substitution, and every wave solves
 // for all of U (the same work on each SIMD, so that U is where the output products need it):
 // an MFMA accumulator lane holds rows 4 g .. 4 g + 3 of a column, exactly the operand of the
 // next 16x16x4 products if contracted index 4 g + e is fed in step e, so U never leaves the
 // registers.
+//
+// Bound by latency, not by its bytes (2 to 6 MB) or products: one trip to memory for all operands, then
+// five dependent phases (gates along the paths, products with S and between nodes, inverses, the
+// solve block by block, outputs) with one wave a SIMD. Measured, 16 key and 32 value heads of 128: 1 node
+// 5.1 us, 16 5.7, 32 6.8, 64 8.8, 65 12.5, 128 15.4.
 //
 // A node whose inputs are not finite must not reach nodes of other paths (0 x NaN in a product
 // of blocks): it is left out, and its outputs and its descendants' set to NaN.

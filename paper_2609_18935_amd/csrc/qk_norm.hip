@@ -12,6 +12,12 @@
 // 8 l + e is the product of two factors that come with the launch) and reduced to
 // [-1/2, 1/2] there, so that a far position loses nothing; sine and cosine of the remaining
 // fraction are fp32. Norm, weight and rotation are fp32, with one rounding to bf16.
+//
+// Inputs are read as streams: each is read once (2,048 tokens of 16 + 2 heads of 256 12.5 -> 11.3 us,
+// and what other kernels left in the caches stays). Outputs are not written so: the attention behind
+// finds them in the caches (4,096 tokens: 292 us for both; 312 with streamed outputs).
+// Measured, 16 + 2 heads of 256, rotated whole: 8,191 tokens 31.5 us (151 MB, 4.8 TB/s, a copy
+// 5.06), 1,000 8.7, one 3.4 (latency: the launch, one trip to memory, one rotation).
 #include "draft.h"
 #include "tailupdate.h"
 
@@ -76,7 +82,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_norm(NormArgs a) {
   const int eb = turns ? half + 8 * l : ea + 8;
 
   // rows (token, head) of the workgroup, head fastest, dealt out to the lane groups; read one
-  // ahead (in place too: a row is written by the lanes that have read it)
+  // ahead (in place too: a row is written by the lanes that have read it; two and more ahead were slower,
+  // 8,191 tokens 38 - 44 us)
   struct Row {
     u32x4 a, b;
   };
