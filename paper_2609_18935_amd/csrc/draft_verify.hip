@@ -58,14 +58,23 @@ __global__ __launch_bounds__(kClearThreads) void k_draft_clear(DraftVerifyArgs a
   if (t < a.n + 2) a.result[t] = t == 0 ? 0 : -1;
 }
 
-// x + the sums of the lanes before it
-__device__ __forceinline__ double wave_scan(double x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
-  return x;
+// x + the value that CTRL moves here from another lane of the rows in MASK (0 elsewhere)
+template <int CTRL, int MASK>
+__device__ __forceinline__ double add_dpp(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, MASK, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, MASK, 0xf, false);
+  return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// x + the values of the lanes before it
+__device__ __forceinline__ double wave_scan(double x) {
+  x = add_dpp<0x111, 0xf>(x);   // row_shr 1, 2, 4, 8: within 16 lanes
+  x = add_dpp<0x112, 0xf>(x);
+  x = add_dpp<0x114, 0xf>(x);
+  x = add_dpp<0x118, 0xf>(x);
+  x = add_dpp<0x142, 0xa>(x);   // the last lane of rows 0 and 2 to rows 1 and 3
+  return add_dpp<0x143, 0xc>(x);   // lane 31 to rows 2 and 3
 }
 
 // 8 elements of a row from t on (0 past its end); `wide`: the address is a multiple of 16
@@ -155,9 +164,8 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
         if (drawn) load_row(Q, t, hi, wide, q);
         x += block_sum(p, q, t);
       }
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
-      if (lane == 0) s_wave[wave] = x;
+      x = wave_scan(x);
+      if (lane == 63) s_wave[wave] = x;
       __syncthreads();
       if (wave == 0) {
         unsigned long long* slots = a.part + (int64_t)pass * a.n_blocks;
@@ -179,7 +187,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
           }
         }
         const double mine = __builtin_bit_cast(double, bits);
-        const double upto = wave_scan(mine, lane);
+        const double upto = wave_scan(mine);
         if (lane < kDrawMaxBlocks) s_before[lane + 1] = upto;
         if (lane == 0) s_before[0] = 0.0;
         const uint64_t some = __ballot(mine > 0.0);
@@ -241,12 +249,8 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
     // the slice that holds the drawn token: the first whose cumulative sum exceeds the target
     // (the last one with a share if u[0] times the whole was rounded up to the whole)
     const double want = (double)a.u[0] * F;
-    int owner = s_last;
-    for (int w = 0; w < a.n_blocks; ++w)
-      if (s_before[w + 1] > want) {
-        owner = w;
-        break;
-      }
+    const uint64_t past = __ballot(lane < a.n_blocks && s_before[lane + 1] > want);
+    const int owner = past ? __builtin_ctzll(past) : s_last;
     if (owner != blk) break;
     double before = s_before[blk];
     int found = -1;
@@ -261,7 +265,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
         if (drawn) load_row(Q, t, hi, wide, q);
       }
       const double x = block_sum(p, q, t);
-      const double cum = wave_scan(x, lane);
+      const double cum = wave_scan(x);
       __syncthreads();
       if (lane == 63) s_wave[wave] = cum;
       __syncthreads();
