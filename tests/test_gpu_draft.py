@@ -150,7 +150,8 @@ def test_attention_ignores_rows_behind_the_draft_and_hidden_nodes():
     assert out[7].isnan().all()
 
 
-@pytest.mark.parametrize("hq,hkv,D,rows,splits", [(16, 2, 256, 50, 0), (8, 2, 128, 700, 0), (16, 4, 64, 90, 1)])
+@pytest.mark.parametrize("hq,hkv,D,rows,splits", [(16, 2, 256, 50, 0), (8, 2, 128, 700, 0), (16, 4, 64, 90, 1),
+                                                    (16, 2, 256, 150, 3), (16, 4, 64, 900, 0)])
 def test_attention_keeps_a_nodes_non_finite_value_from_nodes_that_do_not_see_it(hq, hkv, D, rows, splits):
     rng = np.random.default_rng(D)
     parents = tree("tree", 70)
