@@ -1,6 +1,8 @@
 """Speculative decoding on the GPU beyond the single calls: batches that change the launches'
 shape, stacks of several launches, calls beside each other, drawn shapes, and what the other
 calls of the package read of an accepted path."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -196,3 +198,79 @@ def test_verify_of_drawn_trees(seed):
             u = rng.random(n).astype(np.float32)
             assert _verify(parents, tok, target, u, proposal if drawn else None) == \
                 _want(parents, tok, target, u, proposal if drawn else None)
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of more than 2 GB a buffer: append, attention in one split if the split could, acceptance."""
+    hkv, D, rows, n = 32, 256, 150_000, 3
+    g = torch.Generator(device=DEV).manual_seed(5)
+    kc, vc = (torch.empty(rows + n, hkv, D, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    assert kc.numel() * 2 > 2 ** 31
+    qkv = torch.randn(n, 3 * hkv, D, device=DEV, generator=g).to(torch.bfloat16)
+    p = tu.attn_params(hkv, hkv, D, 0, kv_splits=1)
+    ctx, draft = _ctx(rows, n), tu.Draft([-1, 0, 0])
+    q_hat, out = torch.zeros(2, n, hkv, D, dtype=torch.bfloat16, device=DEV)
+    tu.draft_append(ctx, kc, vc, p, draft, qkv[:, :hkv], qkv[:, hkv:2 * hkv], qkv[:, 2 * hkv:], q_hat)
+    assert torch.equal(q_hat, qkv[:, :hkv]) and torch.equal(kc[rows:], qkv[:, hkv:2 * hkv]) and torch.equal(vc[rows:], qkv[:, 2 * hkv:])
+    ws = tu.draft_attention(ctx, kc, vc, p, draft, q_hat, out)
+    assert ws.numel() > 256 and tu.workspace_faults(ws) == 0          # two splits: one's rows would span 2 GB
+    for i, see in ((0, [0]), (2, [0, 2])):
+        rowset = torch.cat([torch.arange(rows), rows + torch.tensor(see)]).to(DEV)
+        for h in (0, 17, 31):
+            pr = torch.softmax(kc[rowset, h].double() @ q_hat[i, h].double() / 16, 0)
+            V = vc[rowset, h].double()
+            want, mag = pr @ V, pr @ V.abs()
+            err = (out[i, h].double() - want).abs()
+            # output rounding; P and partial outputs in f16, P's subnormals; fp32 scores (|q| |k| <= 20 here) and exponentials
+            assert (err <= BF16 * want.abs() + (2 * 2.0 ** -11 + 2 * (264 * F32 * 20 + 16 * F32)) * mag + 2.0 ** -18).all()
+    layer = tu.LayerIO(tu.TU_LAYER_ATTN, None, None, None, None, k_cache=[kc], v_cache=[vc])
+    tu.draft_accept(ctx, draft, [0, 2], tu.DraftStack([layer], p))
+    assert torch.equal(kc[rows + 1], qkv[2, hkv:2 * hkv]) and torch.equal(vc[rows + 1], qkv[2, 2 * hkv:])
+    assert ctx.pos[rows:rows + 2].tolist() == [rows, rows + 1]
+
+
+def test_probability_rows_that_lie_far_apart():
+    rng = np.random.default_rng(6)
+    V, step, parents = 700, 1 << 30, [-1, 0, 0]
+    target = rows_of(rng, 3, V, 1.0)
+    far = torch.empty(2 * step + V, device=DEV).as_strided((3, V), (step, 1))
+    far.copy_(torch.from_numpy(target))
+    tok = drafted(rng, parents, target, distinct=True)
+    for s in range(4):
+        u = np.random.default_rng(s).random(3).astype(np.float32)
+        got = tu.draft_verify(tu.Draft(parents), torch.from_numpy(tok).to(DEV), far, torch.from_numpy(u).to(DEV))
+        assert got.tolist() == _want(parents, tok, target, u)
+
+
+def test_steps_from_two_threads():
+    setups = [_step_setup(5), _step_setup(6, rows=77, n=40)]
+    want = [_step(s) for s in setups]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                got = _step(setups[i])
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+def test_kernel_times_carry_the_calls_names():
+    s = _step_setup(7)
+    tu.profile_enable(True)
+    try:
+        _step(s)
+        names = set(tu.profile_collect())
+    finally:
+        tu.profile_enable(False)
+    assert {"qk_norm_rope", "draft_attention", "draft_merge", "draft_conv", "draft_delta", "draft_verify"} <= names
