@@ -55,8 +55,10 @@ def _resources(remarks: str) -> dict:
 # splitting it in equal accumulator and vector halves; the delta rule's direct chain is
 # spared 90 register moves per chunk, the probe's score passes one per score.
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=true"]
+# The first arguments of a kernel come with its waves, in scalar registers, instead of from memory.
+_PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=14"]
 FILE_FLAGS = {"attention.hip": _VGPR_MFMA, "delta.hip": _VGPR_MFMA, "probe.hip": _VGPR_MFMA,
-              "draft_attention.hip": _VGPR_MFMA, "draft_recurrent.hip": _VGPR_MFMA}
+              "draft_attention.hip": [*_VGPR_MFMA, *_PRELOAD], "draft_recurrent.hip": _VGPR_MFMA}
 
 
 def _compile(src: str):

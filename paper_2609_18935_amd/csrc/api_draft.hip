@@ -288,9 +288,6 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     const int keys = draft_stage_keys(p->head_dim), stages = (int)((seq->len + n + keys - 1) / keys);
     a.split_stages = stages / splits;
     a.more_stages = stages % splits;
-    a.inv_tiles = 1.f / a.n_tiles;
-    a.inv_splits = 1.f / splits;
-    a.inv_group = 1.f / a.group;
     if ((int64_t)p->n_kv_heads * splits * a.n_tiles >= 1 << 21 || n * a.group >= 1 << 21)   // quotient() in the kernel
       return fail(TU_ERR_ARG, "too many heads");
     a.scale_log2 = p->softmax_scale * 1.4426950408889634f;

@@ -55,9 +55,6 @@ struct DraftAttnArgs {
   int32_t group;          // query heads per KV head
   int32_t split_stages;   // stages of a split; the first more_stages splits have one more
   int32_t more_stages;
-  float inv_tiles;        // reciprocals
-  float inv_splits;
-  float inv_group;
   float scale_log2;       // softmax_scale * log2(e)
   int32_t n_waves;        // ceil(n * G / 32): waves with rows
   DraftMasks seen;

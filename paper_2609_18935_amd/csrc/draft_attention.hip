@@ -75,8 +75,9 @@ __device__ __forceinline__ u32x4 buffer_of(const void* base, uint32_t bytes) {
                (uint32_t)__builtin_amdgcn_readfirstlane(bytes), (uint32_t)kBufWord3};
 }
 
-// x / d for 0 <= x < 2^21, inv = 1 / d: the half keeps the product off every border
-__device__ __forceinline__ int quotient(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
+// x / d for 0 <= x < 2^21: the half keeps the product off every border (the reciprocal's and the product's
+// errors, 1.5 * 2^-23 of it, move it by less than x 2^-22 / d < 1 / (2 d))
+__device__ __forceinline__ int quotient(int x, int d) { return (int)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)d)); }
 
 // Barrier that does not wait for the loads in flight.
 __device__ __forceinline__ void wg_barrier() {
@@ -86,8 +87,13 @@ __device__ __forceinline__ void wg_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Workgroups of a launch: a whole number per die (xcd_remap).
+__host__ __device__ constexpr int whole_dies(int items) { return (items + kXcds - 1) / kXcds * kXcds; }
+
 template <int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_draft_attn(DraftAttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_draft_attn(
+    const bf16_t* k_cache, const bf16_t* v_cache, const bf16_t* q_hat, int len, int n, int Hkv, int G, int n_splits, int n_tiles,
+    int split_stages, int more_stages, DraftAttnArgs a) {   // up to `a`: in registers from the start
   constexpr int NS = D / 16;                 // 16-dim steps of S^T = K Q^T
   constexpr int NDB = D / 32;                // 32-dim blocks of O^T
   constexpr int RC = D / 8;                  // 16-byte chunks per row
@@ -106,22 +112,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ unsigned long long s_spoilt[D][2];   // nodes whose value is not finite in f16, by dim
   __shared__ int s_spoils;
 
-  const int item = xcd_remap(blockIdx.x, gridDim.x);
-  const int Hq = a.n_q_heads, Hkv = a.n_kv_heads;
-  if (item >= Hkv * a.n_splits * a.n_tiles) return;
-  status_mark(a.status);
+  const int items = Hkv * n_splits * n_tiles;
+  const int item = xcd_remap(blockIdx.x, whole_dies(items));
+  if (item >= items) return;
   // the row tiles of one key range are neighbours: they share a die's L2
-  const int range = __builtin_amdgcn_readfirstlane(quotient(item, a.inv_tiles));
-  const int tile = __builtin_amdgcn_readfirstlane(item - range * a.n_tiles);
-  const int hkv = __builtin_amdgcn_readfirstlane(quotient(range, a.inv_splits));
-  const int split = __builtin_amdgcn_readfirstlane(range - hkv * a.n_splits);
-  const int len = a.len, n = a.n, G = a.group;
+  const int range = __builtin_amdgcn_readfirstlane(quotient(item, n_tiles));
+  const int tile = __builtin_amdgcn_readfirstlane(item - range * n_tiles);
+  const int hkv = __builtin_amdgcn_readfirstlane(quotient(range, n_splits));
+  const int split = __builtin_amdgcn_readfirstlane(range - hkv * n_splits);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hl = lane >> 5, col = lane & 31;
   // stages u0 .. u1 - 1: equal shares, the first `more_stages` splits one more
-  const int u0 = split * a.split_stages + min(split, a.more_stages);
-  const int u1 = u0 + a.split_stages + (split < a.more_stages ? 1 : 0);
+  const int u0 = split * split_stages + min(split, more_stages);
+  const int u1 = u0 + split_stages + (split < more_stages ? 1 : 0);
   const int rs = Hkv * D;   // elements of a cache row
 
   // ---- a stage: LDS chunk i * 512 + tid is loaded by load i of the thread. The resources start
@@ -132,7 +136,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   static_assert(LR % (KSWZ + 1) == 0 && LR % 4 == 0, "the loads of a thread take the same chunk");
   const long start = (long)u0 * SK * rs + (long)hkv * D;
   const uint32_t bytes = (uint32_t)(min((u1 - u0) * SK, len + n - u0 * SK) * rs * 2 - (rs - D) * 2);
-  const u32x4 kres = buffer_of(a.k_cache + start, bytes), vres = buffer_of(a.v_cache + start, bytes);
+  const u32x4 kres = buffer_of(k_cache + start, bytes), vres = buffer_of(v_cache + start, bytes);
   uint32_t koff, voff;   // of the next stage to load
   {
     const int lrow = tid / RC, lc = tid % RC;
@@ -155,6 +159,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   // the first stages are asked for before anything else; Q is waited for with the first of them
   load_k(0);
+  const int Hq = Hkv * G;
   const int rows_total = n * G;
   const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
   // Q's rows are read a line at a time (four parts of a row, 64 / LPR rows a load) and go
@@ -167,13 +172,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   uint64_t mask = 0;
   if (busy) {
     const int r = tile * kDraftRows + wave * 32 + col;
-    const int node = min(quotient(r, a.inv_group), n - 1);
+    const int node = min(quotient(r, G), n - 1);
     const int row = r < rows_total ? node * Hq + hkv * G + (r - node * G) : -1;
     if (hl == 0) s_row[wave * 32 + col] = row;
     const bf16_t* from[QL];
 #pragma unroll
     for (int i = 0; i < QL; ++i)
-      from[i] = a.q_hat + (long)max(s_row[wave * 32 + lane / LPR + i * (64 / LPR)], 0) * D + (lane % LPR) * 8;
+      from[i] = q_hat + (long)max(s_row[wave * 32 + lane / LPR + i * (64 / LPR)], 0) * D + (lane % LPR) * 8;
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -188,6 +193,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   load_k(1);
   load_v(1);
   load_k(2);
+  status_mark(a.status);
   if (busy) {
     if (u1 * SK > len) s_mask[wave * 32 + col][hl] = mask;
     char* const mine = (wave < 4 ? g_k : g_v) + 3 * UB + (wave & 3) * (UB / 4);
@@ -442,7 +448,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                                                     __builtin_bit_cast(uint32_t, l_run), false, false);
   const float l_tot = __builtin_bit_cast(float, (uint32_t)lsw[0]) + __builtin_bit_cast(float, (uint32_t)lsw[1]);
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;   // 0: no key of this split is seen; NaN goes on
-  const bool whole = a.n_splits == 1;
+  const bool whole = n_splits == 1;
   const int row = s_row[wave * 32 + col_e];
   if (u1 * SK > len && s_spoils) {
     const uint64_t m0 = s_mask[wave * 32 + col_e][0], m1 = s_mask[wave * 32 + col_e][1];
@@ -474,7 +480,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       __builtin_amdgcn_raw_buffer_store_b128(xy, res, lane_e * 16 + p * 1024, 0, kWriteThrough);
     }
     if (hl_e == 0) {
-      float* ml = a.part_ml + ((long)((hkv * a.n_waves + tile * (kDraftRows / 32) + wave) * 32 + col_e) * a.n_splits + split) * 2;
+      float* ml = a.part_ml + ((long)((hkv * a.n_waves + tile * (kDraftRows / 32) + wave) * 32 + col_e) * n_splits + split) * 2;
       ml[0] = l_tot == 0.f ? -__builtin_inff() : m_run == -__builtin_inff() ? 0.f : m_run;
       ml[1] = l_tot;
     }
@@ -574,15 +580,18 @@ __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) 
 
 hipError_t launch_draft_attention(const DraftAttnArgs& a, int head_dim, hipStream_t s) {
   const int items = a.n_kv_heads * a.n_splits * a.n_tiles;
-  const int blocks = (items + kXcds - 1) / kXcds * kXcds;   // a whole number per die (xcd_remap)
   if (items <= 0) return hipSuccess;
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(whole_dies(items)), dim3(kThreads), 0, s, a.k_cache, a.v_cache, a.q_hat, a.len, a.n,
+                       a.n_kv_heads, a.group, a.n_splits, a.n_tiles, a.split_stages, a.more_stages, a);
+    return hipGetLastError();
+  };
   switch (head_dim) {
-    case 256: hipLaunchKernelGGL(k_draft_attn<256>, dim3(blocks), dim3(kThreads), 0, s, a); break;
-    case 128: hipLaunchKernelGGL(k_draft_attn<128>, dim3(blocks), dim3(kThreads), 0, s, a); break;
-    case 64: hipLaunchKernelGGL(k_draft_attn<64>, dim3(blocks), dim3(kThreads), 0, s, a); break;
+    case 256: return run(k_draft_attn<256>);
+    case 128: return run(k_draft_attn<128>);
+    case 64: return run(k_draft_attn<64>);
     default: return hipErrorInvalidValue;
   }
-  return hipGetLastError();
 }
 
 hipError_t launch_draft_merge(const DraftAttnArgs& a, int head_dim, hipStream_t s) {
