@@ -58,7 +58,7 @@ _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=true"]
 # The first arguments of a kernel come with its waves, in scalar registers, instead of from memory.
 _PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=14"]
 FILE_FLAGS = {"attention.hip": _VGPR_MFMA, "delta.hip": _VGPR_MFMA, "probe.hip": _VGPR_MFMA,
-              "draft_attention.hip": [*_VGPR_MFMA, *_PRELOAD], "draft_recurrent.hip": _VGPR_MFMA}
+              "draft_attention.hip": [*_VGPR_MFMA, *_PRELOAD], "draft_recurrent.hip": [*_VGPR_MFMA, *_PRELOAD]}
 
 
 def _compile(src: str):

@@ -30,7 +30,7 @@
 // Bound by latency, not by its bytes (2 to 6 MB) or products: one trip to memory for all operands, then
 // five dependent phases (gates along the paths, products with S and between nodes, inverses, the
 // solve block by block, outputs) with one wave a SIMD. Measured, 16 key and 32 value heads of 128: 1 node
-// 5.1 us, 16 5.7, 32 6.8, 64 8.8, 65 12.5, 128 15.4.
+// 4.9 us, 16 5.4, 32 6.6, 64 8.3, 65 12.0, 128 14.8.
 //
 // A node whose inputs are not finite must not reach nodes of other paths (0 x NaN in a product
 // of blocks): it is left out, and its outputs and its descendants' set to NaN.
@@ -125,7 +125,9 @@ __device__ __forceinline__ double add_dpp(double x) {
 constexpr int tri(int b) { return b * (b + 1) / 2; }
 
 template <int DK, int NB>   // NB: blocks of 16 nodes
-__global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
+__global__ __launch_bounds__(kThreads) void k_draft_delta(
+    const float* state, const bf16_t* q, const bf16_t* k, const bf16_t* v, const float* beta, const float* gate_in, int n,
+    uint32_t heads, DraftDeltaArgs a) {   // up to `a`: in registers from the start
   constexpr int NK = DK / 32;               // 32-deep steps of a row product
   constexpr int NSL = DK / kBlock;          // workgroups of a head
   constexpr int N = NB * kBlock;
@@ -146,12 +148,11 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   __shared__ float s_beta[N];
   __shared__ unsigned long long s_bad[kBlock][2];   // nodes to leave out, for each state row
 
-  const int Hv = a.n_v_heads, Hk = a.n_k_heads;
-  const int item = xcd_remap(blockIdx.x, gridDim.x);
+  const int Hk = heads & 0xFFFF, Hv = heads >> 16;
+  const int item = xcd_remap(blockIdx.x, Hv * NSL);
   if (item >= Hv * NSL) return;
   const int h = item / NSL, kh = h / (Hv / Hk);
   const int i0 = (item - h * NSL) * kBlock;
-  const int n = a.n;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, col = lane & 15;
@@ -163,12 +164,12 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
   if (tid < n) {
     see0 = a.seen.m[tid][0];
     see1 = a.seen.m[tid][1];
-    gin = a.g[(long)tid * Hv + h];
-    bin = a.beta[(long)tid * Hv + h];
+    gin = gate_in[(long)tid * Hv + h];
+    bin = beta[(long)tid * Hv + h];
   }
   float sx[8];   // wave s takes dims 32 s .. of S
   if (wave < NK) {
-    const float* sp = a.state + ((long)h * DK + i0 + col) * DK + 8 * g + 32 * wave;
+    const float* sp = state + ((long)h * DK + i0 + col) * DK + 8 * g + 32 * wave;
     *(f32x4*)sx = *(const f32x4*)sp;
     *(f32x4*)(sx + 4) = *(const f32x4*)(sp + 4);
   }
@@ -181,13 +182,13 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
     const long at = ((long)min(b * kBlock + col, n - 1) * Hk + kh) * DK + 8 * g;   // rows past the last repeat it
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
-      kf[rb][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a.k + at + 32 * s));
-      qf[rb][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(a.q + at + 32 * s));
+      kf[rb][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(k + at + 32 * s));
+      qf[rb][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(q + at + 32 * s));
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = b * kBlock + 4 * g + e;
-      vf[rb][e] = bf16_to_f32(a.v[((long)min(i, n - 1) * Hv + h) * DK + i0 + col]);
+      vf[rb][e] = bf16_to_f32(v[((long)min(i, n - 1) * Hv + h) * DK + i0 + col]);
     }
   }
   // a thread's share of a node's path: PARTS neighbouring lanes a node
@@ -407,11 +408,16 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(DraftDeltaArgs a) {
 template <int DK>
 hipError_t delta_for(const DraftDeltaArgs& a, hipStream_t s) {
   const int blocks = (a.n_v_heads * (DK / kBlock) + 7) & ~7;   // xcd_remap wants a multiple of 8
-  if (a.n <= 16) hipLaunchKernelGGL((k_draft_delta<DK, 1>), dim3(blocks), dim3(kThreads), 0, s, a);
-  else if (a.n <= 32) hipLaunchKernelGGL((k_draft_delta<DK, 2>), dim3(blocks), dim3(kThreads), 0, s, a);
-  else if (a.n <= 64) hipLaunchKernelGGL((k_draft_delta<DK, 4>), dim3(blocks), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((k_draft_delta<DK, 8>), dim3(blocks), dim3(kThreads), 0, s, a);
-  return hipGetLastError();
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, s, a.state, a.q, a.k, a.v, a.beta, a.g, a.n,
+                       (uint32_t)a.n_k_heads | (uint32_t)a.n_v_heads << 16, a);
+    return hipGetLastError();
+  };
+  if (a.n_v_heads > UINT16_MAX) return hipErrorInvalidValue;
+  if (a.n <= 16) return run(k_draft_delta<DK, 1>);
+  if (a.n <= 32) return run(k_draft_delta<DK, 2>);
+  if (a.n <= 64) return run(k_draft_delta<DK, 4>);
+  return run(k_draft_delta<DK, 8>);
 }
 
 }  // namespace
