@@ -516,27 +516,40 @@ constexpr int kMergeGroups = kMergeThreads / 16;
 constexpr int kMergeEach = kMaxDraftSplits / kMergeGroups;   // splits of a lane group
 static_assert(kMergeThreads / 32 == kMergeRows && kMaxDraftSplits == 4 * 32, "32 lanes form a row's weights");
 
+// `op` over 32 lanes, the same bits in each of them
+template <class Op>
+__device__ __forceinline__ float over_32(float x, Op op) {
+  const auto moved = [&](auto ctrl) __attribute__((always_inline)) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x = op(x, moved(IntC<0xB1>{}));    // quad_perm 1,0,3,2
+  x = op(x, moved(IntC<0x4E>{}));    // quad_perm 2,3,0,1
+  x = op(x, moved(IntC<0x141>{}));   // row_half_mirror
+  x = op(x, moved(IntC<0x140>{}));   // row_mirror
+  return op(x, __shfl_xor(x, 16, 64));
+}
+
 template <int D>
-__global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) {
+__global__ __launch_bounds__(kMergeThreads) void k_draft_merge(const _Float16* part_o, const float* part_ml, bf16_t* to,
+                                                               int n, int G, int Hkv, int ns, int n_waves) {
   constexpr int PIECES = D / 16;
   __shared__ float s_w[kMergeRows][kMaxDraftSplits + 1], s_l[kMergeRows];
   __shared__ __attribute__((aligned(16))) float s_o[kMergeGroups][kMergeRows][20];
-  const int rows = a.n * a.group;
+  const int rows = n * G;
   const int piece = blockIdx.x / 4 % PIECES, part = blockIdx.x / (4 * PIECES);   // the four parts of a piece are neighbours
-  const int hkv = part / a.n_waves, r0 = (part - hkv * a.n_waves) * 32 + blockIdx.x % 4 * kMergeRows;
+  const int hkv = part / n_waves, r0 = (part - hkv * n_waves) * 32 + blockIdx.x % 4 * kMergeRows;
   if (r0 >= rows) return;
   const int tid = threadIdx.x, g = tid >> 4, col = tid & 7, hl = tid >> 3 & 1;
-  const int ns = a.n_splits;
 
   typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
   const int wr = tid >> 5, wl = tid & 31;   // forms weights of row r0 + wr
   f32x2 x[4];
-  const f32x2* ml = (const f32x2*)a.part_ml + ((long)hkv * a.n_waves * 32 + r0 + wr) * ns;
+  const f32x2* ml = (const f32x2*)part_ml + ((long)hkv * n_waves * 32 + r0 + wr) * ns;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     x[i] = r0 + wr < rows && wl + 32 * i < ns ? ml[wl + 32 * i] : f32x2{-__builtin_inff(), 0.f};
-  const _Float16* po = a.part_o + ((long)hkv * a.n_waves + r0 / 32) * 32 * D + piece * 512 + (hl * 32 + r0 % 32 + col) * 8;
-  const long each = (long)a.n_kv_heads * a.n_waves * 32 * D;   // of a split
+  const _Float16* po = part_o + ((long)hkv * n_waves + r0 / 32) * 32 * D + piece * 512 + (hl * 32 + r0 % 32 + col) * 8;
+  const long each = (long)Hkv * n_waves * 32 * D;   // of a split
   f16x8 v[kMergeEach];
 #pragma unroll
   for (int i = 0; i < kMergeEach; ++i) {
@@ -544,8 +557,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) 
     v[i] = s < ns && r0 + col < rows ? *(const f16x8*)(po + s * each) : f16x8{};
   }
   float M = fmaxf(fmaxf(x[0][0], x[1][0]), fmaxf(x[2][0], x[3][0]));
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
+  M = over_32(M, [](float a, float b) { return fmaxf(a, b); });
   float L = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -553,8 +565,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) 
     s_w[wr][wl + 32 * i] = w;   // 0 past the last split
     L += w;
   }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) L += __shfl_xor(L, d, 64);
+  L = over_32(L, [](float a, float b) { return a + b; });
   if (wl == 0) s_l[wr] = L;
   __syncthreads();
   float acc[8] = {};
@@ -572,8 +583,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_draft_merge(DraftAttnArgs a) 
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < kMergeGroups; ++i) sum += s_o[i][out][d];
-  const int node = r / a.group;
-  ((__bf16*)a.out)[((long)node * a.n_q_heads + hkv * a.group + (r - node * a.group)) * D + 16 * piece + d] = (__bf16)(sum / s_l[out]);
+  const int node = r / G;
+  ((__bf16*)to)[((long)(node * Hkv + hkv) * G + (r - node * G)) * D + 16 * piece + d] = (__bf16)(sum / s_l[out]);
 }
 
 }  // namespace
@@ -597,13 +608,17 @@ hipError_t launch_draft_attention(const DraftAttnArgs& a, int head_dim, hipStrea
 hipError_t launch_draft_merge(const DraftAttnArgs& a, int head_dim, hipStream_t s) {
   const int parts = a.n_kv_heads * a.n_waves * 4;
   if (parts <= 0) return hipSuccess;
+  const auto run = [&](auto kernel, int pieces) {
+    hipLaunchKernelGGL(kernel, dim3(parts * pieces), dim3(kMergeThreads), 0, s, a.part_o, a.part_ml, a.out, a.n, a.group,
+                       a.n_kv_heads, a.n_splits, a.n_waves);
+    return hipGetLastError();
+  };
   switch (head_dim) {
-    case 256: hipLaunchKernelGGL(k_draft_merge<256>, dim3(parts * 16), dim3(kMergeThreads), 0, s, a); break;
-    case 128: hipLaunchKernelGGL(k_draft_merge<128>, dim3(parts * 8), dim3(kMergeThreads), 0, s, a); break;
-    case 64: hipLaunchKernelGGL(k_draft_merge<64>, dim3(parts * 4), dim3(kMergeThreads), 0, s, a); break;
+    case 256: return run(k_draft_merge<256>, 16);
+    case 128: return run(k_draft_merge<128>, 8);
+    case 64: return run(k_draft_merge<64>, 4);
     default: return hipErrorInvalidValue;
   }
-  return hipGetLastError();
 }
 
 }  // namespace tu
