@@ -28,10 +28,10 @@
 // node's mask to the unit and drops the keys whose bit is clear.
 //
 // Measured with heads 16 / 2 of 256: 64 nodes over 65,536 rows 70 us (135 MB, 69 GFLOP) + 8 for the
-// join, about 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an 8192^3 bf16 matrix product sustains here;
+// join (34 MB of partial outputs), about 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an 8192^3 bf16 matrix product sustains here;
 // the matrix cores are busy in 53 % of all cycles, 62 % within the loop): bound by the matrix cores at the clock
-// that the power allows. One node over 32,768 rows 15 us + 4: HBM (67 MB, 4.4 TB/s). 24
-// nodes over 11,907 rows 15 + 5: Q (96 KB a workgroup) and its partial outputs (96 KB) cost as much as the
+// that the power allows. One node over 32,768 rows 15 us + 3: HBM (67 MB, 4.4 TB/s). 24
+// nodes over 11,907 rows 15 + 4.4: Q (96 KB a workgroup) and its partial outputs (96 KB) cost as much as the
 // five stages between them. One node over 300 rows 9 us with the join: latency.
 #include "attention_tile.h"
 #include "draft.h"
