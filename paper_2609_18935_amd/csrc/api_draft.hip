@@ -88,29 +88,51 @@ void norm_record(const tu_attn_params* p, const tu_qk_norm* norm, int64_t T, Nor
   a->part_heads = (heads + a->head_parts - 1) / a->head_parts;
 }
 
-// Workgroups of the attention kernel over the key range: at most one per CU, as they need all of its
-// LDS. A stage of a split takes about as long as 2.6 MB of partial outputs on their way through memory,
-// so stages * (splits' partial outputs) is least at the root below: 24 nodes of 16 + 2 heads of 256
-// over 3,000 rows 95 splits of one stage 21.8 us, 32 of three 17.3, 16 of six 19.9; one node 95 splits 10.4, 48 10.7.
-// Up to three stages more than a split's are no reason to split: the join costs a launch (64 nodes over
-// no rows, two stages: 11.2 us in one split, 15.3 in two; 24 nodes over 100 rows, four: 12.3 and 12.8; over
-// 200 rows, seven: 16.1 and 12.9).
-int draft_splits(const tu_attn_params* p, int64_t n, int64_t len) {
-  const int64_t G = p->n_q_heads / p->n_kv_heads;
-  const int64_t tiles = (n * G + kDraftRows - 1) / kDraftRows;
-  const int64_t keys = draft_stage_keys(p->head_dim), stages = (len + n + keys - 1) / keys;
-  int64_t want = p->kv_splits;
-  if (want == 0) {
-    const int64_t most = std::max<int64_t>(1, kCus / (p->n_kv_heads * std::max<int64_t>(1, tiles)));
-    const double partial = n * p->n_q_heads * p->head_dim * 2.0 / 2.6e6;   // of a split, in stages
-    const int64_t least = (stages + most - 1) / most, each = (int64_t)(std::sqrt(stages * partial) + 0.4);
-    want = stages <= std::max(least, each) + 3 ? 1 : each > least ? (stages + each - 1) / each : most;
+// Splits of the key range and rows of a workgroup (in waves of 32) of the attention, by their estimated time.
+// A workgroup holds a CU. In microseconds, as fitted to launches over 0 to 50,000 rows, trees of 1 to 128
+// nodes and four head layouts (the choice is within 1 % of the best measured one in the mean): a stage takes 1.0 +
+// 0.03 a wave with rows (0.7 of that with head_dim 64, whose stages are half as long), a wave's queries and outputs 0.1,
+// those of a second wave on a SIMD 0.6, the join's launch 2.8 and its partial outputs a microsecond for 2 MB on
+// their way through memory; what the tiles read again costs one for 40 MB. So short contexts take one split and small tiles (16 + 2 heads of 256, 64
+// nodes over 40 rows: 9.9 us in 16 tiles of one wave, 14.4 in two of eight, 15.1 with four splits), long ones
+// one tile and a split for every CU (64 nodes over 24,000 rows: 41.4 us in two tiles of eight waves, 43.5 in
+// four of four; 24 nodes over 3,000: 14.2 in three tiles of two and 32 splits, 17.3 in one of six, 21.4 with 95 splits).
+struct DraftPlan {
+  int splits;
+  int tile_waves;
+};
+
+DraftPlan draft_plan(const tu_attn_params* p, int64_t n, int64_t len) {
+  const int64_t Hkv = p->n_kv_heads, waves = std::max<int64_t>(1, (n * (p->n_q_heads / Hkv) + 31) / 32);
+  const int64_t keys = draft_stage_keys(p->head_dim), stages = std::max<int64_t>(1, (len + n + keys - 1) / keys);
+  // a split's rows span less than 2^31 bytes (its loads' offsets are 32 bits wide), with the stages loaded past its end
+  const int64_t stage_bytes = keys * Hkv * p->head_dim * 2;
+  const int64_t fewest = (stages * stage_bytes) / (INT32_MAX - 8 * stage_bytes) + 1;
+  const double partial = n * p->n_q_heads * p->head_dim * 2.0 / 2.0e6;   // of a split
+  const double half = p->head_dim == 64 ? 0.7 : 1.0, read = (p->head_dim == 64 ? 16 : 32) * 1024 / 40.0e6;   // of a stage
+  DraftPlan best{1, 1};
+  double least = 0.0;
+  for (int64_t w = 1; w <= std::min<int64_t>(waves, kDraftRows / 32); ++w) {
+    const int64_t tiles = (waves + w - 1) / w;
+    if ((waves + tiles - 1) / tiles != w) continue;   // as many tiles of fewer waves do
+    const double stage = (1.0 + 0.03 * w) * half;
+    const double rows = 0.1 * std::min<int64_t>(w, 4) + 0.6 * std::max<int64_t>(0, w - 4);
+    // stages of a split: with k of them the time is k stage + (stages / k) partial, but one workgroup a CU
+    const int64_t most = std::max<int64_t>(1, kCus / (Hkv * tiles)), k0 = (stages + most - 1) / most;
+    const int64_t k = std::max(k0, (int64_t)(std::sqrt(stages * partial / stage) + 0.5));
+    const int64_t many = p->kv_splits > 0 ? p->kv_splits : k == k0 ? most : (stages + k - 1) / k;
+    for (const int64_t want : {many, p->kv_splits > 0 ? many : (int64_t)1}) {
+      const int64_t s = std::max<int64_t>(1, std::min<int64_t>({std::max(want, fewest), stages, kMaxDraftSplits}));
+      const int64_t turns = (Hkv * tiles * s + kCus - 1) / kCus;
+      const double time = turns * (rows + (stages + s - 1) / s * stage) + (s > 1 ? 2.8 + s * partial : 0.0) +
+                          Hkv * tiles * stages * read;
+      if (least == 0.0 || time < least) {
+        least = time;
+        best = {(int)s, (int)w};
+      }
+    }
   }
-  // a split's rows span less than 2^31 bytes (its loads' offsets are 32 bits wide), with the
-  // stages loaded past its end
-  const int64_t stage_bytes = keys * p->n_kv_heads * p->head_dim * 2;
-  want = std::max(want, (stages * stage_bytes) / (INT32_MAX - 8 * stage_bytes) + 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, stages, kMaxDraftSplits}));
+  return best;
 }
 
 // Partial rows of a split: those of whole waves.
@@ -243,7 +265,7 @@ int draft_append(const tu_seq* seq, void* k_cache, void* v_cache, const tu_attn_
 
 size_t draft_attention_workspace_size(const tu_attn_params* p, int32_t n, int64_t len) {
   if (check_attn(p) || n < 0 || n > TU_MAX_DRAFT || len < 0 || len > INT32_MAX / 2) return 0;
-  return attention_ws(p, n, draft_splits(p, n, len));
+  return attention_ws(p, n, draft_plan(p, n, len).splits);
 }
 
 int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache, const tu_attn_params* p,
@@ -263,7 +285,8 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     if (!k_cache || !v_cache || !q_hat || !out) return fail(TU_ERR_ARG, "null tensor");
     if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q_hat) || !aligned16(out))
       return fail(TU_ERR_ARG, "tensors must be 16-byte aligned");
-    const int splits = draft_splits(p, n, seq->len);
+    const DraftPlan plan = draft_plan(p, n, seq->len);
+    const int splits = plan.splits;
     if (int e = check_workspace(workspace, workspace_bytes, attention_ws(p, n, splits))) return e;
     DraftAttnArgs a{};
     a.q_hat = static_cast<const bf16_t*>(q_hat);
@@ -282,8 +305,9 @@ int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache,
     a.n_q_heads = p->n_q_heads;
     a.n_kv_heads = p->n_kv_heads;
     a.group = p->n_q_heads / p->n_kv_heads;
-    a.n_tiles = (n * a.group + kDraftRows - 1) / kDraftRows;
     a.n_waves = (n * a.group + 31) / 32;
+    a.tile_waves = plan.tile_waves;
+    a.n_tiles = (a.n_waves + plan.tile_waves - 1) / plan.tile_waves;
     a.n_splits = splits;
     const int keys = draft_stage_keys(p->head_dim), stages = (int)((seq->len + n + keys - 1) / keys);
     a.split_stages = stages / splits;

@@ -50,7 +50,8 @@ struct DraftAttnArgs {
   int32_t n;
   int32_t n_q_heads;
   int32_t n_kv_heads;
-  int32_t n_tiles;        // ceil(n * G / kDraftRows)
+  int32_t n_tiles;        // row tiles of a KV head
+  int32_t tile_waves;     // waves of a tile that have rows, 32 each
   int32_t n_splits;
   int32_t group;          // query heads per KV head
   int32_t split_stages;   // stages of a split; the first more_stages splits have one more

@@ -92,8 +92,8 @@ __host__ __device__ constexpr int whole_dies(int items) { return (items + kXcds 
 
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_draft_attn(
-    const bf16_t* k_cache, const bf16_t* v_cache, const bf16_t* q_hat, int len, int n, int Hkv, int G, int n_splits, int n_tiles,
-    int split_stages, int more_stages, DraftAttnArgs a) {   // up to `a`: in registers from the start
+    const bf16_t* k_cache, const bf16_t* v_cache, const bf16_t* q_hat, int len, int n, int Hkv, int G, int n_splits,
+    uint32_t tiles, int split_stages, int more_stages, DraftAttnArgs a) {   // up to `a`: in registers from the start
   constexpr int NS = D / 16;                 // 16-dim steps of S^T = K Q^T
   constexpr int NDB = D / 32;                // 32-dim blocks of O^T
   constexpr int RC = D / 8;                  // 16-byte chunks per row
@@ -112,6 +112,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ unsigned long long s_spoilt[D][2];   // nodes whose value is not finite in f16, by dim
   __shared__ int s_spoils;
 
+  const int n_tiles = tiles & 0xFFFFFF, tile_waves = tiles >> 24;
   const int items = Hkv * n_splits * n_tiles;
   const int item = xcd_remap(blockIdx.x, whole_dies(items));
   if (item >= items) return;
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   load_k(0);
   const int Hq = Hkv * G;
   const int rows_total = n * G;
-  const bool busy = tile * kDraftRows + wave * 32 < rows_total;   // a wave without rows only loads
+  const int first = (tile * tile_waves + wave) * 32;   // of this wave's packed rows
+  const bool busy = wave < tile_waves && first < rows_total;   // a wave without rows only loads
   // Q's rows are read a line at a time (four parts of a row, 64 / LPR rows a load) and go
   // through the wave's own LDS, in a ring place that is free until the first step, into the
   // operands: lane (query, half) holds 8 dims of each 16.
@@ -171,7 +173,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   u32x4 w[NS];
   uint64_t mask = 0;
   if (busy) {
-    const int r = tile * kDraftRows + wave * 32 + col;
+    const int r = first + col;
     const int node = min(quotient(r, G), n - 1);
     const int row = r < rows_total ? node * Hq + hkv * G + (r - node * G) : -1;
     if (hl == 0) s_row[wave * 32 + col] = row;
@@ -471,7 +473,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // otherwise be written back when the kernel ends, with nothing else to do (24 nodes over 11,907
     // rows, 25 MB of partial outputs: 22.0 -> 21.1 us with the join; 64 over 65,536: 83.8 -> 82.8).
     if (row < 0) return;
-    const long at = (long)(split * Hkv + hkv) * a.n_waves + tile * (kDraftRows / 32) + wave;
+    const int packed = tile * tile_waves + wave;
+    const long at = (long)(split * Hkv + hkv) * a.n_waves + packed;
     const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(a.part_o + at * 32 * D, 0, 64 * D, kBufWord3);
 #pragma unroll
     for (int p = 0; p < 2 * NDB; ++p) {
@@ -480,7 +483,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       __builtin_amdgcn_raw_buffer_store_b128(xy, res, lane_e * 16 + p * 1024, 0, kWriteThrough);
     }
     if (hl_e == 0) {
-      float* ml = a.part_ml + ((long)((hkv * a.n_waves + tile * (kDraftRows / 32) + wave) * 32 + col_e) * n_splits + split) * 2;
+      float* ml = a.part_ml + ((long)((hkv * a.n_waves + packed) * 32 + col_e) * n_splits + split) * 2;
       ml[0] = l_tot == 0.f ? -__builtin_inff() : m_run == -__builtin_inff() ? 0.f : m_run;
       ml[1] = l_tot;
     }
@@ -594,7 +597,8 @@ hipError_t launch_draft_attention(const DraftAttnArgs& a, int head_dim, hipStrea
   if (items <= 0) return hipSuccess;
   const auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(whole_dies(items)), dim3(kThreads), 0, s, a.k_cache, a.v_cache, a.q_hat, a.len, a.n,
-                       a.n_kv_heads, a.group, a.n_splits, a.n_tiles, a.split_stages, a.more_stages, a);
+                       a.n_kv_heads, a.group, a.n_splits, (uint32_t)a.n_tiles | (uint32_t)a.tile_waves << 24,
+                       a.split_stages, a.more_stages, a);
     return hipGetLastError();
   };
   switch (head_dim) {

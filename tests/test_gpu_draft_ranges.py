@@ -274,3 +274,25 @@ def test_kernel_times_carry_the_calls_names():
     finally:
         tu.profile_enable(False)
     assert {"qk_norm_rope", "draft_attention", "draft_merge", "draft_conv", "draft_delta", "draft_verify"} <= names
+
+
+@pytest.mark.parametrize("hq,hkv,D,rows,n", [(16, 2, 256, 40000, 64), (16, 2, 256, 40000, 27), (16, 2, 256, 30000, 40),
+                                             (32, 8, 128, 25000, 61), (16, 4, 64, 60000, 128), (8, 1, 64, 50000, 33)])
+def test_attention_with_many_rows_a_workgroup(hq, hkv, D, rows, n):
+    """Long caches, where a workgroup takes five to eight waves of rows."""
+    parents = tree("tree", n, 3)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    k, v = torch.randn(2, rows + n, hkv, D, device=DEV, generator=g).to(torch.bfloat16)
+    q = torch.randn(n, hq, D, device=DEV, generator=g).to(torch.bfloat16)
+    out = torch.full((n + 1, hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    tu.draft_attention(_ctx(rows, n), k, v, tu.attn_params(hq, hkv, D), tu.Draft(parents), q, out[:n])
+    assert (out[n] == 7).all()
+    for i in (0, n // 2, n - 1):
+        see = torch.cat([torch.arange(rows), rows + torch.tensor(O.line(parents, i))]).to(DEV)
+        for h in range(hq):
+            pr = torch.softmax(k[see, h * hkv // hq].double() @ q[i, h].double() * D ** -0.5, 0)
+            V = v[see, h * hkv // hq].double()
+            want, mag = pr @ V, pr @ V.abs()
+            err = (out[i, h].double() - want).abs()
+            # as over 150,000 rows above
+            assert (err <= BF16 * want.abs() + (2 * 2.0 ** -11 + 2 * ((D + 8) * F32 * 20 + 16 * F32)) * mag + 2.0 ** -18).all()
