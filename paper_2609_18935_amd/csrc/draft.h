@@ -61,7 +61,7 @@ struct DraftAttnArgs {
   DraftMasks seen;
 };
 constexpr int kMaxDraftSplits = 128;
-constexpr int kDraftRows = 256;         // packed query rows of an attention workgroup
+constexpr int kDraftRows = 256;         // packed query rows of an attention workgroup, at most
 constexpr int kDraftUnit = 32;          // keys of a unit of the products
 // Keys of a stage: 16 KB of K, 16 KB of V; half of that with head_dim 64, where longer stages leave
 // short contexts too few of them.

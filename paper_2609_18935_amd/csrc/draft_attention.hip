@@ -2,7 +2,7 @@
 // ancestors' rows and its own.
 //
 // The G query heads of a KV head are packed as rows (row = node * G + h mod G). A workgroup
-// takes 256 rows (8 waves of 32, two per SIMD) of one KV head and one split of the key range.
+// takes up to 256 rows (8 waves of 32, two per SIMD) of one KV head and one split of the key range.
 // K and V come as they lie in the cache, in stages of 16 KB each (32 keys of 256 dims), by LDS
 // DMA into rings of four, two to three of them in flight: the cache is asked for far ahead whatever
 // the number of rows, and waves without rows only load.
@@ -31,8 +31,9 @@
 // join (34 MB of partial outputs), about 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an 8192^3 bf16 matrix product sustains here;
 // the matrix cores are busy in 53 % of all cycles, 62 % within the loop): bound by the matrix cores at the clock
 // that the power allows. One node over 32,768 rows 15 us + 3: HBM (67 MB, 4.4 TB/s). 24
-// nodes over 11,907 rows 15 + 4.4: Q (96 KB a workgroup) and its partial outputs (96 KB) cost as much as the
-// five stages between them. One node over 300 rows 9 us with the join: latency.
+// nodes over 11,907 rows 14 + 4 (two tiles of 96 rows, 64 splits): Q (48 KB a workgroup) and its partial
+// outputs (48 KB) cost half as much as the six stages between them. One node over 300 rows 8.4 us with the
+// join, 24 9.6, without cached rows 6.3: latency.
 #include "attention_tile.h"
 #include "draft.h"
 
