@@ -30,7 +30,7 @@
 // Bound by latency, not by its bytes (2 to 6 MB) or products: one trip to memory for all operands, then
 // five dependent phases (gates along the paths, products with S and between nodes, inverses, the
 // solve block by block, outputs) with one wave a SIMD. Measured, 16 key and 32 value heads of 128: 1 node
-// 4.9 us, 16 5.4, 32 6.6, 64 8.3, 65 12.0, 128 14.8.
+// 4.6 us, 7 5.0, 16 5.4, 32 6.4, 64 8.2, 65 12.1, 128 14.9.
 //
 // A node whose inputs are not finite must not reach nodes of other paths (0 x NaN in a product
 // of blocks): it is left out, and its outputs and its descendants' set to NaN.
@@ -359,18 +359,22 @@ __global__ __launch_bounds__(kThreads) void k_draft_delta(
   if (tid < N) {
     const int b = tid >> 4;
     const float* mb = s_m[tri(b) + b];
+    f32x4 m[kBlock][4];   // all of it first: a row's reads would hold up its step
+#pragma unroll
+    for (int i = 1; i < kBlock; ++i)
+#pragma unroll
+      for (int j = 0; j < i; j += 4) m[i][j / 4] = *(const f32x4*)(mb + i * kMStride + j);
+    asm volatile("" ::: "memory");
     float t[kBlock];
 #pragma unroll
     for (int i = 0; i < kBlock; ++i) {
-      float x[4] = {i == col ? 1.f : 0.f, 0.f, 0.f, 0.f};
+      t[i] = i == col ? 1.f : 0.f;
+      if (NB > 1 || i < n) {   // rows of no node are zeros but for the one
+        float x[4] = {t[i], 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < i; j += 4) {
-        const f32x4 m = *(const f32x4*)(mb + i * kMStride + j);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (j + e < i) x[e] = __builtin_fmaf(m[e], t[j + e], x[e]);
+        for (int j = 0; j < i; ++j) x[j & 3] = __builtin_fmaf(m[i][j / 4][j & 3], t[j], x[j & 3]);
+        t[i] = (x[0] + x[1]) + (x[2] + x[3]);
       }
-      t[i] = (x[0] + x[1]) + (x[2] + x[3]);
       s_t[b][i * kMStride + col] = t[i];
     }
   }
