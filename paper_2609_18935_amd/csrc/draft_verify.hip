@@ -77,7 +77,7 @@ __device__ __forceinline__ double wave_scan(double x) {
   return add_dpp<0x143, 0xc>(x);   // lane 31 to rows 2 and 3
 }
 
-// 8 elements of a row from t on (0 past its end); `wide`: the address is a multiple of 16
+// 8 elements of a row from t on (0 from hi on, and no reads there); `wide`: the address is a multiple of 16
 __device__ __forceinline__ void load_row(const float* row, int64_t t, int64_t hi, bool wide, float (&x)[kDrawPer]) {
   static_assert(kDrawPer == 8, "two vectors");
   if (wide && t + kDrawPer <= hi) {
@@ -85,10 +85,16 @@ __device__ __forceinline__ void load_row(const float* row, int64_t t, int64_t hi
     *(f32x4*)(x + 4) = *(const f32x4*)(row + t + 4);
   } else {
 #pragma unroll
-    for (int j = 0; j < kDrawPer; ++j) x[j] = t + j < hi ? row[t + j] : 0.f;
+    for (int j = 0; j < kDrawPer; ++j) {
+      const float y = row[min(t + j, hi - 1)];
+      x[j] = t + j < hi ? y : 0.f;
+    }
   }
 }
 
+// DRAWN: the drafter's probabilities are given. (Two instances: the code runs once, and much of the
+// time goes into fetching it.)
+template <bool DRAWN>
 __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) {
   __shared__ Odds s_odds[kMaxDraft];
   __shared__ uint64_t s_seen[kMaxDraft][2];
@@ -100,7 +106,6 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
   __shared__ int s_last, s_expired;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = a.n, blk = blockIdx.x;
-  const bool drawn = a.proposal != nullptr;
 
   if (tid < 2) s_first[tid] = 0;
   if (tid == 0) s_expired = 0;
@@ -131,38 +136,39 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
     __syncthreads();
     const int m = s_on[1] ? 127 - __builtin_clzll(s_on[1]) : 63 - __builtin_clzll(s_on[0]);
     const float* P = a.target + m * a.target_stride;
-    const float* Q = drawn ? a.proposal + m * a.proposal_stride : nullptr;
+    const float* Q = DRAWN ? a.proposal + m * a.proposal_stride : nullptr;
     float pr[kDrawPer], qr[kDrawPer] = {};
     load_row(P, t0, hi, wide, pr);
-    if (drawn) load_row(Q, t0, hi, wide, qr);
+    if (DRAWN) load_row(Q, t0, hi, wide, qr);
 
     double b = 0.0, F = 1.0;
     int n_out = 0, n_mine = 0;
-    // the value of element t of what is left, given the rejected tokens that may be t
-    auto left = [&](float p, float q, int64_t t, const int* out, int n_out) __attribute__((always_inline)) -> double {
-      if (drawn) {
-        const double v = (double)p - b * (double)q;
-        return v > 0.0 ? v : 0.0;
-      }
-      for (int k = 0; k < n_out; ++k)
-        if (out[k] == t) return 0.0;
-      return p > 0.f ? (double)p : 0.0;
-    };
-    // this thread's part of block t - lo of the slice, in element order
-    auto block_sum = [&](const float (&p)[kDrawPer], const float (&q)[kDrawPer], int64_t t) __attribute__((always_inline)) -> double {
+    // 8 values of what is left, from element t on, and their sum in element order
+    auto left = [&](const float (&p)[kDrawPer], const float (&q)[kDrawPer], int64_t t, double (&v)[kDrawPer])
+                    __attribute__((always_inline)) -> double {
+      uint32_t gone = 0;   // rejected tokens among them
+      if constexpr (!DRAWN)
+        for (int k = 0; k < n_mine; ++k) {
+          const int64_t at = s_mine[k] - t;
+          if (at >= 0 && at < kDrawPer) gone |= 1u << at;
+        }
       double x = 0.0;
 #pragma unroll
-      for (int j = 0; j < kDrawPer; ++j) x += left(p[j], q[j], t + j, s_mine, n_mine);
+      for (int j = 0; j < kDrawPer; ++j) {
+        v[j] = DRAWN ? (double)p[j] - b * (double)q[j] : gone >> j & 1 ? 0.0 : (double)p[j];
+        v[j] = v[j] > 0.0 ? v[j] : 0.0;
+        x += v[j];
+      }
       return x;
     };
     // sum of what is left over the whole row, the same in every workgroup
     auto total = [&]() -> double {
-      double x = block_sum(pr, qr, t0);
+      double v[kDrawPer], x = left(pr, qr, t0, v);
       for (int64_t t = t0 + kDrawThreads * kDrawPer; t < hi; t += kDrawThreads * kDrawPer) {
         float p[kDrawPer], q[kDrawPer] = {};
         load_row(P, t, hi, wide, p);
-        if (drawn) load_row(Q, t, hi, wide, q);
-        x += block_sum(p, q, t);
+        if (DRAWN) load_row(Q, t, hi, wide, q);
+        x += left(p, q, t, v);
       }
       x = wave_scan(x);
       if (lane == 63) s_wave[wave] = x;
@@ -203,11 +209,17 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
     for (int c = s_child[m]; c > 0 && took < 0; c = s_sibling[c]) {
       const Odds o = s_odds[c];
       double px = 0.0;
-      if (o.token >= 0) px = left(o.p, o.q, o.token, s_out, n_out);
+      if (o.token >= 0) {
+        px = DRAWN ? (double)o.p - b * (double)o.q : (double)o.p;
+        if (!(px > 0.0)) px = 0.0;
+        if constexpr (!DRAWN)
+          for (int k = 0; k < n_out; ++k)
+            if (s_out[k] == o.token) px = 0.0;
+      }
       if ((double)o.u * (double)o.q * F < px) {
         took = c;
       } else {
-        if (drawn) {
+        if constexpr (DRAWN) {
           b += F;
         } else {
           const bool mine = o.token >= lo && o.token < hi;
@@ -262,9 +274,10 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
         for (int j = 0; j < kDrawPer; ++j) p[j] = pr[j], q[j] = qr[j];
       } else {
         load_row(P, t, hi, wide, p);
-        if (drawn) load_row(Q, t, hi, wide, q);
+        if (DRAWN) load_row(Q, t, hi, wide, q);
       }
-      const double x = block_sum(p, q, t);
+      double v[kDrawPer];
+      const double x = left(p, q, t, v);
       const double cum = wave_scan(x);
       __syncthreads();
       if (lane == 63) s_wave[wave] = cum;
@@ -279,9 +292,8 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
       int first = -1, last = -1;
 #pragma unroll
       for (int j = 0; j < kDrawPer; ++j) {
-        const double v = left(p[j], q[j], t + j, s_mine, n_mine);
-        sum += v;
-        if (v > 0.0) {
+        sum += v[j];
+        if (v[j] > 0.0) {
           last = (int)(t + j);
           if (first < 0 && sum > want) first = last;
         }
@@ -318,7 +330,8 @@ hipError_t launch_draft_clear(const DraftVerifyArgs& a, hipStream_t s) {
 
 hipError_t launch_draft_draw(const DraftVerifyArgs& a, hipStream_t s) {
   if (a.n_blocks < 1 || a.n_blocks > kDrawMaxBlocks) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_draft_draw, dim3(a.n_blocks), dim3(kDrawThreads), 0, s, a);
+  if (a.proposal) hipLaunchKernelGGL(k_draft_draw<true>, dim3(a.n_blocks), dim3(kDrawThreads), 0, s, a);
+  else hipLaunchKernelGGL(k_draft_draw<false>, dim3(a.n_blocks), dim3(kDrawThreads), 0, s, a);
   return hipGetLastError();
 }
 
