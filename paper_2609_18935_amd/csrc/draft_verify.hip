@@ -205,20 +205,22 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
     };
 
     int took = -1;
-    bool tried = false;
-    for (int c = s_child[m]; c > 0 && took < 0; c = s_sibling[c]) {
-      const Odds o = s_odds[c];
-      double px = 0.0;
-      if (o.token >= 0) {
-        px = DRAWN ? (double)o.p - b * (double)o.q : (double)o.p;
-        if (!(px > 0.0)) px = 0.0;
-        if constexpr (!DRAWN)
-          for (int k = 0; k < n_out; ++k)
-            if (s_out[k] == o.token) px = 0.0;
-      }
-      if ((double)o.u * (double)o.q * F < px) {
-        took = c;
-      } else {
+    bool summed = false, whole = false;   // F is a sum; of the row itself
+    for (int c = s_child[m];;) {
+      if (c > 0) {
+        const Odds o = s_odds[c];
+        double px = 0.0;
+        if (o.token >= 0) {
+          px = DRAWN ? (double)o.p - b * (double)o.q : (double)o.p;
+          if (!(px > 0.0)) px = 0.0;
+          if constexpr (!DRAWN)
+            for (int k = 0; k < n_out; ++k)
+              if (s_out[k] == o.token) px = 0.0;
+        }
+        if ((double)o.u * (double)o.q * F < px) {
+          took = c;
+          break;
+        }
         if constexpr (DRAWN) {
           b += F;
         } else {
@@ -232,10 +234,16 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
           ++n_out;
           n_mine += mine;
         }
-        F = total();
-        tried = true;
-        if (s_expired) break;
+        c = s_sibling[c];
+      } else if (summed) {
+        if (F > 0.0 || whole) break;
+        b = 0.0;   // nothing left: the row itself
+        n_mine = 0;
+        whole = true;
       }
+      F = total();
+      summed = true;
+      if (s_expired) break;
     }
     if (s_expired) break;
     if (took >= 0) {
@@ -244,13 +252,6 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
       __syncthreads();
       continue;
     }
-    if (!tried) F = total();                 // a leaf
-    if (!(F > 0.0) && !s_expired) {          // nothing left: the row itself
-      b = 0.0;
-      n_mine = 0;
-      F = total();
-    }
-    if (s_expired) break;
     if (blk == 0 && tid < n && (s_on[tid >> 6] >> (tid & 63) & 1)) {   // the path, in order
       const uint64_t below = (1ull << (tid & 63)) - 1;
       const int at = __popcll(s_on[0] & (tid < 64 ? below : ~0ull)) + (tid < 64 ? 0 : __popcll(s_on[1] & below));
