@@ -14,8 +14,9 @@
 // the few workgroups fit the chip many times over) and adds all of them up in one order. The
 // workgroup whose slice holds the drawn token finds it. Bound by latency: the odds (two
 // dependent loads), the rows of a node (a load; a megabyte, kept in registers over its passes)
-// and one exchange a pass. Measured over a vocabulary of 131,072: 7.6 us for one node, 8.4 for a chain of
-// six, 12.3 for 64 nodes with several rejections (k_draft_clear 1.4 of it), 17.9 without proposals.
+// and one exchange a pass; and by fetching code that runs once, so it is kept small. Measured over a
+// vocabulary of 131,072: 7.5 us for one node, 7.9 for a chain of six, 11.5 for 64 nodes with several
+// rejections (k_draft_clear 1.4 of it), 16.6 without proposals.
 #include <algorithm>
 
 #include "draft.h"
@@ -305,15 +306,13 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
       if (has ? lane == __builtin_ctzll(has) : lane == 0) s_pick[0][wave] = has ? first : -1;
       if (share ? lane == 63 - __builtin_clzll(share) : lane == 0) s_pick[1][wave] = share ? last : -1;
       __syncthreads();
-      int hit = -1;
-      for (int w = kWaves - 1; w >= 0; --w) {
-        if (s_pick[0][w] >= 0) hit = s_pick[0][w];
-        found = max(found, s_pick[1][w]);
-      }
-      if (hit >= 0) {
-        found = hit;
+      const int hit = lane < kWaves ? s_pick[0][lane] : -1, near = lane < kWaves ? s_pick[1][lane] : -1;
+      const uint64_t hits = __ballot(hit >= 0), nears = __ballot(near >= 0);
+      if (hits) {
+        found = __builtin_amdgcn_readlane(hit, __builtin_ctzll(hits));
         break;
       }
+      if (nears) found = __builtin_amdgcn_readlane(near, 63 - __builtin_clzll(nears));
     }
     if (tid == 0) a.result[1] = found;
     break;
