@@ -55,14 +55,17 @@ struct IntC {
   static constexpr int value = B;
 };
 
-// 16 bytes per lane from the buffer at voff + soff to LDS at lds + 16 lane. Written out, so that
+// 16 bytes per lane from the buffer at voff to LDS at lds + 16 lane. Written out, so that
 // one loop body can serve every place of the rings: for the compiler's own load it would wait
 // for all loads in flight before any LDS read whose address it cannot tell apart. It has no
 // output register; the kernel waits for it by count, and for all of them before it ends.
-__device__ __forceinline__ void dma_lds(uint32_t lds, uint32_t voff, u32x4 res, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+// The whole offset is the vector one: the range check compares it with the resource's size
+// itself, while a scalar offset larger than a short split's rows would leave the check to a
+// difference that is negative.
+__device__ __forceinline__ void dma_lds(uint32_t lds, uint32_t voff, u32x4 res) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"(lds), "v"(voff), "s"(res), "s"(soff)
+               : "s"(lds), "v"(voff), "s"(res)
                : "memory", "m0");
 }
 
@@ -150,12 +153,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const uint32_t lds_v = (uint32_t)(uintptr_t)(lds_void*)g_v + wave * 1024;
   auto load_k = [&](int place) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) dma_lds(lds_k + place * UB + i * kThreads * 16, koff, kres, i * LR * rs * 2);
+    for (int i = 0; i < NL; ++i) dma_lds(lds_k + place * UB + i * kThreads * 16, koff + i * LR * rs * 2, kres);
     koff += stage_bytes;
   };
   auto load_v = [&](int place) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) dma_lds(lds_v + place * UB + i * kThreads * 16, voff, vres, i * LR * rs * 2);
+    for (int i = 0; i < NL; ++i) dma_lds(lds_v + place * UB + i * kThreads * 16, voff + i * LR * rs * 2, vres);
     voff += stage_bytes;
   };
 
