@@ -1,11 +1,13 @@
 """Speculative decoding on the GPU at the limits of its inputs, against the float64 definitions: rows
-behind a short split."""
+behind a short split, scores far apart."""
 import numpy as np
 import pytest
 import torch
 
-from draft_cases import bf16, tree, worst
-from test_gpu_draft import _attn
+import paper_2609_18935_amd as tu
+from oracle import draft as O
+from draft_cases import BF16, F16, F32, bf16, f64, tree, worst
+from test_gpu_draft import DEV, _attn, _ctx, dev
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +24,31 @@ def test_attention_ignores_rows_behind_a_split_shorter_than_a_stage(hq, hkv, D, 
     kv[:, rows + n:] = float("nan")
     out, want, bound, _ = _attn(hq, hkv, D, rows, tree("tree", n), kv=kv, spare=spare, splits=splits)
     assert worst(out, want, bound) <= 1
+
+
+@pytest.mark.parametrize("hq,hkv,D", [(16, 2, 256), (8, 2, 128), (16, 4, 64)])
+@pytest.mark.parametrize("rows,splits", [(4000, 1), (4000, 0), (700, 1), (12000, 3)])
+@pytest.mark.parametrize("gap", [14.0, 16.0, 17.5, 18.0])
+def test_attention_beside_a_sink(hq, hkv, D, rows, splits, gap):
+    """The first key's score lies `gap` above all others' (in units of e) and its value is zero: the output is what
+    the many small probabilities leave."""
+    rng = np.random.default_rng([D, rows, int(2 * gap)])
+    n = 5
+    k, v = bf16(rng, 2, rows + n + 3, hkv, D)
+    q = bf16(rng, n, hq, D, scale=0.5)
+    k[..., 0], q[..., 0] = 0, gap * D ** 0.5 / 8
+    k[0], k[0, :, 0] = 0, 8
+    v = v.abs()
+    v[0] = 0
+    parents = tree("tree", n)
+    out = torch.full((n, hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = tu.draft_attention(_ctx(rows, n, spare=3), dev(k), dev(v), tu.attn_params(hq, hkv, D, kv_splits=splits), tu.Draft(parents),
+                            dev(q), out)
+    want, mag, most = O.draft_attention(f64(q), f64(k)[:rows + n], f64(v)[:rows + n], parents, D ** -0.5)
+    assert want.max() < 2e-2 and want.min() > 1e-6
+    # the output's rounding; P and the partial outputs in f16; the scores' fp32 sums and the exponential, in numerator and
+    # denominator. Below f16's normal range: P, at most 2^-25 of 2^11 times the largest key's; partial outputs, 2^-25
+    bound = BF16 * np.abs(want) + (2 * F16 + 2 * ((D + 8) * F32 * most[..., None] + 16 * F32)) * mag + \
+        2.0 ** -36 * (rows + n) * f64(v).max() + 2.0 ** -25
+    assert worst(out, want, bound) <= 1
+    assert tu.workspace_faults(ws) == 0
