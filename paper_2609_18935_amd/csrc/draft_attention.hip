@@ -460,8 +460,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const auto lsw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, l_run),
                                                     __builtin_bit_cast(uint32_t, l_run), false, false);
   const float l_tot = __builtin_bit_cast(float, (uint32_t)lsw[0]) + __builtin_bit_cast(float, (uint32_t)lsw[1]);
-  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;   // 0: no key of this split is seen; NaN goes on
   const bool whole = n_splits == 1;
+  // 0: no key of this split is seen. A query sees its own key: over all keys a sum of 0 (scores of -infinity
+  // alone) is NaN, as where splits are joined
+  const float inv = l_tot == 0.f && !whole ? 0.f : 1.f / l_tot;
   const int row = s_row[wave * 32 + col_e];
   if (u1 * SK > len && s_spoils) {
     const uint64_t m0 = s_mask[wave * 32 + col_e][0], m1 = s_mask[wave * 32 + col_e][1];

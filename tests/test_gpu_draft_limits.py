@@ -1,5 +1,5 @@
 """Speculative decoding on the GPU at the limits of its inputs, against the float64 definitions: rows
-behind a short split, scores far apart."""
+behind a short split, scores far apart, queries that are not finite."""
 import numpy as np
 import pytest
 import torch
@@ -52,3 +52,24 @@ def test_attention_beside_a_sink(hq, hkv, D, rows, splits, gap):
         2.0 ** -36 * (rows + n) * f64(v).max() + 2.0 ** -25
     assert worst(out, want, bound) <= 1
     assert tu.workspace_faults(ws) == 0
+
+
+@pytest.mark.parametrize("hq,hkv,D,rows,n,splits", [(16, 2, 256, 0, 1, 0), (16, 2, 256, 40, 9, 1), (16, 2, 256, 900, 9, 0),
+                                                    (8, 2, 128, 40, 9, 1), (8, 2, 128, 500, 9, 4), (16, 4, 64, 0, 1, 0),
+                                                    (16, 4, 64, 300, 9, 1)])
+def test_attention_of_queries_that_are_not_finite(hq, hkv, D, rows, n, splits):
+    """Scores of -infinity alone, of both infinities, and NaN: softmax is NaN in each, whatever the splits, and
+    the other queries do not notice."""
+    rng = np.random.default_rng([D, rows])
+    k, v = bf16(rng, 2, rows + n + 3, hkv, D)
+    q, parents = bf16(rng, n, hq, D), tree("tree", n)
+    k[..., 3] = 1
+    clean, last = q.clone(), n - 1
+    q[last, 0, 3], q[last, 1, 3], q[last, hq - 1, 5] = -float("inf"), float("inf"), float("nan")
+    out = torch.full((n, hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    tu.draft_attention(_ctx(rows, n, spare=3), dev(k), dev(v), tu.attn_params(hq, hkv, D, kv_splits=splits), tu.Draft(parents),
+                       dev(q), out)
+    want, mag, most = O.draft_attention(f64(clean), f64(k)[:rows + n], f64(v)[:rows + n], parents, D ** -0.5)
+    want[last, [0, 1, hq - 1]] = np.nan
+    bound = BF16 * np.abs(want) + (2 * F16 + 2 * ((D + 8) * F32 * most[..., None] + 16 * F32)) * mag + 2.0 ** -25
+    assert worst(out, want, bound) <= 1
