@@ -48,7 +48,7 @@
 extern "C" {
 #endif
 
-#define TU_ABI_VERSION 6
+#define TU_ABI_VERSION 7
 
 #define TU_OK 0
 #define TU_ERR_ARG (-1)       /* null pointer, unsupported or inconsistent shape */
@@ -555,8 +555,14 @@ int draft_append(const tu_seq* seq, void* k_cache, void* v_cache, const tu_attn_
  * 2^16 or more). A node's key or value that is not finite (or beyond f16) reaches only the nodes that see it. The
  * result does not depend on rows behind the last node. p->kv_splits as in
  * tail_prefill_attention (more where a split's rows would span 2 GB).
+ * draft_attention_workspace_size is what a call with this n and len needs: splits and rows of
+ * a workgroup are chosen together, so a smaller draft or a shorter context can need more.
+ * draft_attention_workspace_bound is enough for every draft of at most max_n nodes over at
+ * most max_len rows: the size for a workspace that a program keeps. Both return 0 for invalid
+ * arguments.
  */
 size_t draft_attention_workspace_size(const tu_attn_params* p, int32_t n, int64_t len);
+size_t draft_attention_workspace_bound(const tu_attn_params* p, int32_t max_n, int64_t max_len);
 int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache, const tu_attn_params* p,
                     const tu_draft* draft, const void* q_hat, void* out, void* workspace, size_t workspace_bytes,
                     void* stream);

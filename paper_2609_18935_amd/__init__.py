@@ -34,6 +34,7 @@ from .binding import (  # noqa: F401
     draft_accept,
     draft_append,
     draft_attention,
+    draft_attention_workspace_bound,
     draft_attention_workspace_size,
     draft_delta_rule,
     draft_short_conv,

@@ -129,6 +129,7 @@ _SIGNATURES = {
     "draft_append": (_i32, [ctypes.POINTER(tu_seq), _vp, _vp, ctypes.POINTER(tu_attn_params), ctypes.POINTER(tu_qk_norm),
                             ctypes.POINTER(tu_draft), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
     "draft_attention_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(tu_attn_params), _i32, _i64]),
+    "draft_attention_workspace_bound": (ctypes.c_size_t, [ctypes.POINTER(tu_attn_params), _i32, _i64]),
     "draft_attention": (_i32, [ctypes.POINTER(tu_seq), _vp, _vp, ctypes.POINTER(tu_attn_params),
                                ctypes.POINTER(tu_draft), _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "draft_short_conv": (_i32, [ctypes.POINTER(tu_draft), ctypes.POINTER(tu_conv_tensor), _i32, _i32, _i32, _vp]),
@@ -147,7 +148,7 @@ _SIGNATURES = {
 }
 
 _lib_handle = None
-ABI_VERSION = 6   # TU_ABI_VERSION of include/tailupdate.h that these structures follow
+ABI_VERSION = 7   # TU_ABI_VERSION of include/tailupdate.h that these structures follow
 
 
 def lib():
@@ -673,7 +674,13 @@ def draft_append(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, par
 
 
 def draft_attention_workspace_size(ctx: Context, params: tu_attn_params, draft: Draft) -> int:
+    """Bytes that draft_attention needs for this draft over the context as it is now (a smaller one may need more)."""
     return int(lib().draft_attention_workspace_size(ctypes.byref(params), draft.n, ctx.len))
+
+
+def draft_attention_workspace_bound(params: tu_attn_params, nodes: int, rows: int) -> int:
+    """Bytes that are enough for every draft of at most `nodes` nodes over at most `rows` cache rows."""
+    return int(lib().draft_attention_workspace_bound(ctypes.byref(params), int(nodes), int(rows)))
 
 
 def draft_attention(ctx: Context, k_cache: torch.Tensor, v_cache: torch.Tensor, params: tu_attn_params, draft: Draft,

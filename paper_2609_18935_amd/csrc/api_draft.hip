@@ -144,6 +144,22 @@ size_t attention_ws(const tu_attn_params* p, int64_t n, int splits) {
   return kStatusBytes + align_up(rows * p->head_dim * sizeof(_Float16)) + align_up(rows * 2 * sizeof(float));
 }
 
+// At least attention_ws of every plan for 1 .. n nodes over 0 .. len rows. Neither splits nor rows of a workgroup
+// rise with either number (draft_plan weighs them against each other), so its own formula for the most
+// splits is taken with the fewest tiles and the longest context, for every number of nodes.
+size_t attention_ws_bound(const tu_attn_params* p, int64_t n, int64_t len) {
+  const int64_t Hkv = p->n_kv_heads, keys = draft_stage_keys(p->head_dim), stage_bytes = keys * Hkv * p->head_dim * 2;
+  size_t most = kStatusBytes;
+  for (int64_t i = 1; i <= n; ++i) {
+    const int64_t waves = wave_rows(p, i) / 32 / Hkv, tiles = (waves + kDraftRows / 32 - 1) / (kDraftRows / 32);
+    const int64_t stages = (len + i + keys - 1) / keys;
+    const int64_t fewest = (stages * stage_bytes) / (INT32_MAX - 8 * stage_bytes) + 1;
+    const int64_t many = p->kv_splits > 0 ? p->kv_splits : std::max<int64_t>(1, kCus / (Hkv * tiles));
+    most = std::max(most, attention_ws(p, i, (int)std::min<int64_t>({std::max(many, fewest), stages, kMaxDraftSplits})));
+  }
+  return most;
+}
+
 // The delta kernels' grids and offsets are 32 bits wide.
 int check_delta_heads(const tu_delta_params* p) {
   if (int e = check_delta(p)) return e;
@@ -266,6 +282,11 @@ int draft_append(const tu_seq* seq, void* k_cache, void* v_cache, const tu_attn_
 size_t draft_attention_workspace_size(const tu_attn_params* p, int32_t n, int64_t len) {
   if (check_attn(p) || n < 0 || n > TU_MAX_DRAFT || len < 0 || len > INT32_MAX / 2) return 0;
   return attention_ws(p, n, draft_plan(p, n, len).splits);
+}
+
+size_t draft_attention_workspace_bound(const tu_attn_params* p, int32_t max_n, int64_t max_len) {
+  if (check_attn(p) || max_n < 0 || max_n > TU_MAX_DRAFT || max_len < 0 || max_len > INT32_MAX / 2) return 0;
+  return attention_ws_bound(p, max_n, max_len);
 }
 
 int draft_attention(const tu_seq* seq, const void* k_cache, const void* v_cache, const tu_attn_params* p,

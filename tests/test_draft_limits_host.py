@@ -1,0 +1,46 @@
+"""What a program may keep from one speculative decoding step to the next (host only)."""
+import ctypes
+import random
+
+import pytest
+
+import paper_2609_18935_amd as tu
+from paper_2609_18935_amd import binding as B
+
+
+def _size(p, n, rows):
+    return B.lib().draft_attention_workspace_size(ctypes.byref(p), n, rows)
+
+
+def _drawn(seed):
+    rng = random.Random(seed)
+    hkv = rng.choice([1, 2, 3, 8])
+    return tu.attn_params(hkv * rng.choice([1, 4, 5, 8]), hkv, rng.choice([64, 128, 256]), kv_splits=rng.choice([0, 0, 0, 1, 7, 64]))
+
+
+@pytest.mark.parametrize("p", [tu.attn_params(16, 2, 256), tu.attn_params(32, 8, 128), tu.attn_params(16, 4, 64), tu.attn_params(40, 1, 256),
+                               tu.attn_params(16, 2, 256, kv_splits=5), *[_drawn(s) for s in range(12)]])
+@pytest.mark.parametrize("nodes,rows", [(1, 0), (1, 32768), (24, 2150), (24, 12000), (40, 12000), (128, 70000), (128, 300)])
+def test_one_attention_workspace_serves_every_shorter_context_and_smaller_draft(p, nodes, rows):
+    bound = tu.draft_attention_workspace_bound(p, nodes, rows)
+    lengths = sorted({*range(0, min(rows, 600) + 1, 7), *range(0, rows + 1, max(1, rows // 97)), rows})
+    for n in range(1, nodes + 1):
+        assert max(_size(p, n, r) for r in lengths) <= bound
+
+
+def test_a_context_beyond_32_bit_offsets():
+    p = tu.attn_params(32, 32, 256)        # 16 KB a row: a split takes 131,000 rows
+    bound = tu.draft_attention_workspace_bound(p, 8, 3_000_000)
+    assert all(_size(p, n, r) <= bound for n in range(1, 9) for r in range(0, 3_000_001, 50_000))
+
+
+def test_an_exact_size_is_no_bound():
+    p = tu.attn_params(16, 2, 256)
+    assert _size(p, 24, 2100) > _size(p, 24, 2150)          # the reason for the bound
+
+
+def test_bounds_refused():
+    p, b = tu.attn_params(16, 2, 256), tu.draft_attention_workspace_bound
+    assert b(p, 129, 10) == b(p, -1, 10) == b(p, 4, -1) == b(p, 4, 2 ** 30) == 0
+    assert b(tu.attn_params(16, 3, 256), 4, 10) == 0
+    assert b(p, 0, 10) >= 256

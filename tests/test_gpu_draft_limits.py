@@ -1,5 +1,5 @@
 """Speculative decoding on the GPU at the limits of its inputs, against the float64 definitions: rows
-behind a short split, scores far apart, queries that are not finite."""
+behind a short split, scores far apart, queries that are not finite, a kept workspace."""
 import numpy as np
 import pytest
 import torch
@@ -73,3 +73,17 @@ def test_attention_of_queries_that_are_not_finite(hq, hkv, D, rows, n, splits):
     want[last, [0, 1, hq - 1]] = np.nan
     bound = BF16 * np.abs(want) + (2 * F16 + 2 * ((D + 8) * F32 * most[..., None] + 16 * F32)) * mag + 2.0 ** -25
     assert worst(out, want, bound) <= 1
+
+
+def test_a_workspace_kept_over_steps_of_other_sizes():
+    hq, hkv, D, rng = 16, 2, 256, np.random.default_rng(8)
+    p = tu.attn_params(hq, hkv, D)
+    ws = torch.empty(tu.draft_attention_workspace_bound(p, 40, 2200), dtype=torch.uint8, device=DEV)
+    for rows, n in ((2200, 40), (2100, 24), (2150, 24), (31, 40), (700, 1)):
+        k, v = bf16(rng, 2, rows + n, hkv, D)
+        q, parents = bf16(rng, n, hq, D), tree("tree", n)
+        out = torch.zeros(n, hq, D, dtype=torch.bfloat16, device=DEV)
+        tu.draft_attention(_ctx(rows, n), dev(k), dev(v), p, tu.Draft(parents), dev(q), out, workspace=ws)
+        want, mag, most = O.draft_attention(f64(q), f64(k), f64(v), parents, D ** -0.5)
+        bound = BF16 * np.abs(want) + (2 * F16 + 2 * ((D + 8) * F32 * most[..., None] + 16 * F32)) * mag + 2.0 ** -25
+        assert worst(out, want, bound) <= 1 and tu.workspace_faults(ws) == 0
