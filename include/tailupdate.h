@@ -147,7 +147,9 @@ const char* tu_last_error(void);
  *   TU_FAULT_POSITIONS  d_pos disagrees with the host metadata (`live`, `len`), so
  *                       the update did not remove exactly the rows whose labels lie
  *                       in the ranges;
- *   TU_FAULT_WAIT       a wait of the in-place move expired; moved rows may be wrong;
+ *   TU_FAULT_WAIT       a wait of the in-place move expired; moved rows may be wrong
+ *                       (draft_verify: a wait for other workgroups' sums; its result
+ *                       is whole or empty);
  *   TU_FAULT_RANGE      a value rounded to f16 overflowed; the results are not
  *                       meaningful.
  * tu_workspace_faults enqueues a read of that status on `stream` (the stream the
@@ -609,9 +611,9 @@ int draft_delta_rule(const float* state, const void* q, const void* k, const voi
  *  target, proposal: device fp32 [n] rows of `vocab` values, non-negative, row strides in
  *            elements (at least vocab); tokens: device int32 [n] (a token outside [0, vocab)
  *            is never accepted; tokens[0] is not read); u: device fp32 [n] in [0, 1).
- *  result:   device int32 [n + 2]: accepted nodes (at least 1; 0 only where a wait expired,
- *            TU_FAULT_WAIT), the next token, then the accepted path from node 0 on, filled up
- *            with -1.
+ *  result:   device int32 [n + 2]: accepted nodes (at least 1), the next token, then the
+ *            accepted path from node 0 on, filled up with -1. Where a wait expired it is whole
+ *            or empty (0, then -1 throughout), and TU_FAULT_WAIT is set.
  */
 size_t draft_verify_workspace_size(int32_t n, int64_t vocab);
 int draft_verify(const tu_draft* draft, const int32_t* tokens, const float* target, int64_t target_stride,

@@ -836,7 +836,7 @@ def draft_accept(ctx: Context, draft: Draft, path: Sequence[int], stack: DraftSt
 
 
 TU_FAULT_POSITIONS = 1   # device positions disagreed with the host's live runs
-TU_FAULT_WAIT = 2        # a bounded wait of the in-place move expired
+TU_FAULT_WAIT = 2        # a bounded wait (of the in-place move, of a verification) expired
 TU_FAULT_RANGE = 4       # a value rounded to f16 overflowed
 
 

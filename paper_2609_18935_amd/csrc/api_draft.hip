@@ -457,6 +457,7 @@ int draft_verify(const tu_draft* draft, const int32_t* tokens, const float* targ
     const int64_t block = kDrawThreads * kDrawPer, blocks = (vocab + block - 1) / block;
     a.slice = (blocks + kDrawMaxBlocks - 1) / kDrawMaxBlocks * block;
     a.n_blocks = (int32_t)((vocab + a.slice - 1) / a.slice);
+    a.polls = kDrawPolls;
     a.wide = ((uintptr_t)target & 15) == 0 && target_stride % 4 == 0 &&
              (!proposal || (((uintptr_t)proposal & 15) == 0 && proposal_stride % 4 == 0));
     uint8_t last[kMaxDraft] = {};    // last child so far

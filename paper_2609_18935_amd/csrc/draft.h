@@ -94,6 +94,7 @@ struct DraftDeltaArgs {
 constexpr int kDrawThreads = 512;
 constexpr int kDrawPer = 8;       // consecutive row elements of a thread, in registers
 constexpr int kDrawMaxBlocks = 64;
+constexpr int kDrawPolls = 1 << 20;   // of a wait for another workgroup: many milliseconds
 struct DraftVerifyArgs {
   const int32_t* tokens;
   const float* target;
@@ -109,7 +110,7 @@ struct DraftVerifyArgs {
   int32_t n_blocks;         // workgroups of a pass, each a contiguous slice of the row
   int64_t slice;            // elements of a slice, a multiple of kDrawThreads * kDrawPer
   int32_t wide;             // every row is 16-byte aligned
-  int32_t pad;
+  int32_t polls;            // of a bounded wait, behind the first
   uint64_t first[2];        // nodes that are their parent's first child
   uint8_t parent[kMaxDraft];
   uint8_t child[kMaxDraft];    // first child (0: none)

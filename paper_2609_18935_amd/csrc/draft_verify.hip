@@ -25,7 +25,6 @@ namespace tu {
 
 namespace {
 
-constexpr long kSpinLimit = 1l << 20;   // polls of a bounded wait
 constexpr int kClearThreads = 256;
 static_assert(kDrawMaxBlocks == 64, "a slice's sum per lane");
 constexpr int kWaves = kDrawThreads / 64;
@@ -184,11 +183,11 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
           __hip_atomic_store(slots + blk, bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         unsigned long long bits = 0;   // slices past the last are empty: 0.0
-        long spins = 0;
+        int spins = 0;
         for (;;) {
           if (lane < a.n_blocks) bits = __hip_atomic_load(slots + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           if (__all(bits != kEmpty)) break;
-          if (++spins > kSpinLimit) {
+          if (++spins > a.polls) {
             s_expired = 1;
             break;
           }
@@ -253,19 +252,23 @@ __global__ __launch_bounds__(kDrawThreads) void k_draft_draw(DraftVerifyArgs a) 
       __syncthreads();
       continue;
     }
-    if (blk == 0 && tid < n && (s_on[tid >> 6] >> (tid & 63) & 1)) {   // the path, in order
+    // the slice that holds the drawn token: the first whose cumulative sum exceeds the target
+    // (the last one with a share if u[0] times the whole was rounded up to the whole; without a distribution
+    // there is no token)
+    const bool draws = F > 0.0 && F < __builtin_inf();
+    const double want = (double)a.u[0] * F;
+    const uint64_t past = __ballot(lane < a.n_blocks && s_before[lane + 1] > want);
+    const int owner = !draws ? 0 : past ? __builtin_ctzll(past) : s_last;
+    if (owner != blk) break;
+    // The owner writes all of the result: one whose wait has expired writes nothing, and the count stays 0,
+    // whatever the other workgroups have seen.
+    if (tid < n && (s_on[tid >> 6] >> (tid & 63) & 1)) {   // the path, in order
       const uint64_t below = (1ull << (tid & 63)) - 1;
       const int at = __popcll(s_on[0] & (tid < 64 ? below : ~0ull)) + (tid < 64 ? 0 : __popcll(s_on[1] & below));
       a.result[2 + at] = tid;
       if (tid == m) a.result[0] = at + 1;
     }
-    if (!(F > 0.0 && F < __builtin_inf())) break;   // no distribution: no token
-    // the slice that holds the drawn token: the first whose cumulative sum exceeds the target
-    // (the last one with a share if u[0] times the whole was rounded up to the whole)
-    const double want = (double)a.u[0] * F;
-    const uint64_t past = __ballot(lane < a.n_blocks && s_before[lane + 1] > want);
-    const int owner = past ? __builtin_ctzll(past) : s_last;
-    if (owner != blk) break;
+    if (!draws) break;
     double before = s_before[blk];
     int found = -1;
     for (int64_t tb = lo; tb < hi; tb += kDrawThreads * kDrawPer) {

@@ -1,13 +1,19 @@
 """Speculative decoding on the GPU at the limits of its inputs, against the float64 definitions: rows
-behind a short split, scores far apart, queries that are not finite, a kept workspace."""
+behind a short split, scores far apart, queries that are not finite, a kept workspace,
+waits that expire."""
+import ctypes
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2609_18935_amd as tu
 from oracle import draft as O
-from draft_cases import BF16, F16, F32, bf16, f64, tree, worst
-from test_gpu_draft import DEV, _attn, _ctx, dev
+from paper_2609_18935_amd import binding as B
+from draft_cases import BF16, F16, F32, bf16, f64, rows_of, tree, worst
+from test_gpu_draft import DEV, _attn, _ctx, _want, dev
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +93,52 @@ def test_a_workspace_kept_over_steps_of_other_sizes():
         want, mag, most = O.draft_attention(f64(q), f64(k), f64(v), parents, D ** -0.5)
         bound = BF16 * np.abs(want) + (2 * F16 + 2 * ((D + 8) * F32 * most[..., None] + 16 * F32)) * mag + 2.0 ** -25
         assert worst(out, want, bound) <= 1 and tu.workspace_faults(ws) == 0
+
+
+def _record(name):
+    """The launch record `name` as the library's header declares it."""
+    with open(os.path.join(os.path.dirname(tu.__file__), "csrc", "draft.h")) as f:
+        body = re.search(r"struct %s \{\n(.*?)\n\};" % name, f.read(), re.S).group(1)
+
+    class CallStatus(ctypes.Structure):
+        _fields_ = [("word", ctypes.c_void_p), ("last", ctypes.c_void_p), ("call", ctypes.c_uint32)]
+
+    plain = {"int32_t": ctypes.c_int32, "int64_t": ctypes.c_int64, "uint64_t": ctypes.c_uint64, "uint8_t": ctypes.c_uint8,
+             "CallStatus": CallStatus, "DraftMasks": ctypes.c_uint64 * 2 * 128}
+    fields = []
+    for line in body.splitlines():
+        kind, star, field, count = re.fullmatch(r"\s*(?:const )?([\w ]+?)(\*?) (\w+)(?:\[(\w+)\])?;.*", line).groups()
+        t = ctypes.c_void_p if star else plain[kind]
+        fields.append((field, t * (128 if count == "kMaxDraft" else int(count)) if count else t))
+    return type(name, (ctypes.Structure,), {"_fields_": fields}), CallStatus
+
+
+def test_a_verification_whose_waits_expire_leaves_no_half_result():
+    """Each workgroup looks for the others' sums a few times only: those that come early give up, later ones see them
+    all. The result is whole or empty, and empty only with TU_FAULT_WAIT."""
+    V, lib = 300000, B.lib()
+    target = rows_of(np.random.default_rng(20), 1, V)
+    Args, CallStatus = _record("DraftVerifyArgs")
+    x, t = torch.zeros(1, dtype=torch.int32, device=DEV), torch.from_numpy(target).to(DEV)
+    ws = torch.zeros(tu.draft_verify_workspace_size(tu.Draft([-1]), V), dtype=torch.uint8, device=DEV)
+    result = torch.zeros(3, dtype=torch.int32, device=DEV)
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    us = np.linspace(0, 0.999, 25).astype(np.float32)
+    want = [_want([-1], np.zeros(1, np.int32), target, u[None]) for u in us]
+    seen = []
+    for polls in (0, 1, 2, 3, 4, 6, 8, 12, 16):
+        for i, u in enumerate(us):
+            ud = torch.from_numpy(u[None]).to(DEV)
+            a = Args(tokens=x.data_ptr(), target=t.data_ptr(), proposal=None, u=ud.data_ptr(), result=result.data_ptr(),
+                     target_stride=V, proposal_stride=0, vocab=V, part=ws.data_ptr() + 256,
+                     status=CallStatus(ws.data_ptr(), ws.data_ptr() + 64, 0xF0000000 + len(seen)), n=1, n_blocks=37,
+                     slice=8192, wide=1, polls=polls)
+            a.seen[0][0] = 1
+            assert 36 * a.slice < V <= 37 * a.slice
+            assert lib._ZN2tu18launch_draft_clearERKNS_15DraftVerifyArgsEP12ihipStream_t(ctypes.byref(a), stream) == 0
+            assert lib._ZN2tu17launch_draft_drawERKNS_15DraftVerifyArgsEP12ihipStream_t(ctypes.byref(a), stream) == 0
+            r, fault = result.tolist(), tu.workspace_faults(ws)
+            seen.append((polls, r[0], fault))
+            assert r == want[i] or (r == [0, -1, -1] and fault == tu.TU_FAULT_WAIT), (polls, float(u), r, fault)
+    print("polls, whole results, whole ones beside an expired wait:",
+          [(p, sum(s[1] for s in seen if s[0] == p), sum(s[1] for s in seen if s[0] == p and s[2])) for p in sorted({s[0] for s in seen})])
