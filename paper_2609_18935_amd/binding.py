@@ -759,11 +759,12 @@ def draft_verify(draft: Draft, tokens: torch.Tensor, target: torch.Tensor, unifo
 class DraftStack:
     """The layers and convolutions of a context that an accepted path is kept in (ctypes structs built once,
     reusable as long as the tensors are the same): LayerIO of both kinds (caches, states and the draft's k, v,
-    beta, g) and convs, a sequence of (state [W-1][C], x [n][C]) with one width."""
+    beta, g) and convs, a sequence of (state [W-1][C], x [n][C]) with one width. It holds the tensors that it was
+    built from: a LayerIO that gets others later needs a new stack."""
 
     def __init__(self, layers: Sequence[LayerIO], attn: Optional[tu_attn_params] = None,
                  delta: Optional[tu_delta_params] = None, convs: Sequence = ()):
-        self.attn, self.delta, self._keep = attn, delta, [layers, convs]
+        self.attn, self.delta, self._keep = attn, delta, []
         bf, f32 = torch.bfloat16, torch.float32
         self.device, self.rows, self.capacity, self.width = None, None, None, 1
         tensors = [t for L in layers for t in ((L.k_cache or [None])[0], (L.state or [None])[0]) if t is not None]
@@ -776,8 +777,12 @@ class DraftStack:
                 raise ValueError(f"{what} has {t.shape[0]} rows, other tensors of the draft have {self.rows}")
             self.rows = int(t.shape[0])
 
+        def held(t, what, dtype, shape):
+            self._keep.append(t)
+            return _need(t, what, dtype, shape, self.device)
+
         def one(t, what, dtype, shape):
-            a = (_vp * 1)(_need(t, what, dtype, shape, self.device))
+            a = (_vp * 1)(held(t, what, dtype, shape))
             self._keep.append(a)
             return a
 
@@ -802,10 +807,10 @@ class DraftStack:
                 Hk, Hv, d = delta.n_k_heads, delta.n_v_heads, delta.d_k
                 rows(L.k, "k")
                 c.state = one(L.state[0], "state", f32, (Hv, d, d))
-                c.k = _need(L.k, "k", bf, (self.rows, Hk, d), self.device)
-                c.v = _need(L.v, "v", bf, (self.rows, Hv, d), self.device)
-                c.beta = _need(L.beta, "beta", f32, (self.rows, Hv), self.device)
-                c.g = _need(L.g, "g", f32, (self.rows, Hv), self.device)
+                c.k = held(L.k, "k", bf, (self.rows, Hk, d))
+                c.v = held(L.v, "v", bf, (self.rows, Hv, d))
+                c.beta = held(L.beta, "beta", f32, (self.rows, Hv))
+                c.g = held(L.g, "g", f32, (self.rows, Hv))
         self._convs = (tu_conv_tensor * max(1, len(convs)))()
         self.n_convs = len(convs)
         for i, (st, x) in enumerate(convs):
@@ -814,8 +819,8 @@ class DraftStack:
             self.width = int(st.shape[0]) + 1
             rows(x, "x")
             c = self._convs[i]
-            c.state = _need(st, "state", bf, (self.width - 1, x.shape[1]), self.device)
-            c.x, c.T, c.channels = _need(x, "x", bf, (self.rows, x.shape[1]), self.device), self.rows, int(x.shape[1])
+            c.state = held(st, "state", bf, (self.width - 1, x.shape[1]))
+            c.x, c.T, c.channels = held(x, "x", bf, (self.rows, x.shape[1])), self.rows, int(x.shape[1])
 
 
 def draft_accept(ctx: Context, draft: Draft, path: Sequence[int], stack: DraftStack, stream=None):

@@ -1,8 +1,11 @@
 """What a program may keep from one speculative decoding step to the next (host only)."""
 import ctypes
+import gc
 import random
+import weakref
 
 import pytest
+import torch
 
 import paper_2609_18935_amd as tu
 from paper_2609_18935_amd import binding as B
@@ -44,3 +47,27 @@ def test_bounds_refused():
     assert b(p, 129, 10) == b(p, -1, 10) == b(p, 4, -1) == b(p, 4, 2 ** 30) == 0
     assert b(tu.attn_params(16, 3, 256), 4, 10) == 0
     assert b(p, 0, 10) >= 256
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="host tensors stand in for device tensors")
+def test_a_draft_stack_holds_its_tensors():
+    """A layer that gets a new tensor, or a list that gets a new element, leaves the prepared stack its own."""
+    bf = torch.bfloat16
+    delta = tu.LayerIO(tu.TU_LAYER_DELTA, None, torch.zeros(3, 2, 64, dtype=bf), torch.zeros(3, 4, 64, dtype=bf), None,
+                       state=[torch.zeros(4, 64, 64)], beta=torch.zeros(3, 4), g=torch.zeros(3, 4))
+    attn = tu.LayerIO(tu.TU_LAYER_ATTN, None, None, None, None, k_cache=[torch.zeros(20, 2, 64, dtype=bf)],
+                      v_cache=[torch.zeros(20, 2, 64, dtype=bf)])
+    convs = [(torch.zeros(3, 8, dtype=bf), torch.zeros(3, 8, dtype=bf))]
+    stack = tu.DraftStack([delta, attn], tu.attn_params(4, 2, 64), tu.delta_params(2, 4, 64, 64, 16), convs)
+    given = [delta.k, delta.v, delta.beta, delta.g, delta.state[0], attn.k_cache[0], attn.v_cache[0], *convs[0]]
+    refs, addresses = [weakref.ref(t) for t in given], [t.data_ptr() for t in given]
+    del given
+    delta.k = delta.v = delta.beta = delta.g = None
+    delta.state[0], attn.k_cache[0], attn.v_cache[0], convs[0] = None, None, None, None
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    d, a, c = stack._layers[0], stack._layers[1], stack._convs[0]
+    assert [d.k, d.v, d.beta, d.g, d.state[0], a.k_cache[0], a.v_cache[0], c.state, c.x] == addresses
+    del stack, d, a, c
+    gc.collect()
+    assert all(r() is None for r in refs)
