@@ -481,7 +481,8 @@ class LayerIO:
 
 
 class StackUpdate:
-    """A prepared update_layer_stack call (ctypes structs built once, reusable)."""
+    """A prepared update_layer_stack call (ctypes structs built once, reusable). It holds the tensors that it was
+    built from: a LayerIO that gets others later needs a new one."""
 
     def __init__(self, contexts: Sequence[Context], ranges: Sequence, tails: Sequence[int], layers: Sequence[LayerIO],
                  attn: Optional[tu_attn_params] = None, delta: Optional[tu_delta_params] = None,
@@ -506,6 +507,7 @@ class StackUpdate:
             runs = None if place_runs is None or place_runs[s] is None else place_runs[s]
             rarr, nrr = _ranges_array(runs if runs is not None else [])
             self._keep.append(rarr)
+            self._keep.append(si)
             self._seq_arr[s] = tu_seq_update(ctypes.pointer(ctx.c), arr, nr, int(tails[s]), _ptr(si), parr, npr,
                                              _PLACEMENTS[pl], rarr, nrr)
         self._layer_arr = (tu_layer_io * max(1, len(layers)))()
@@ -514,8 +516,9 @@ class StackUpdate:
                 if ts is None:
                     return None
                 a = (_vp * max(1, n))(*[_ptr(t) for t in ts])
-                self._keep.append(a)
+                self._keep += [a, *ts]
                 return a
+            self._keep += [L.q, L.k, L.v, L.beta, L.g, L.out]
             self._layer_arr[l] = tu_layer_io(L.kind, plist(L.k_cache), plist(L.v_cache),
                                              plist(getattr(L, "vt_cache", None)), plist(L.state), _ptr(L.q),
                                              _ptr(L.k), _ptr(L.v), _ptr(L.beta), _ptr(L.g), _ptr(L.out))

@@ -1,4 +1,4 @@
-"""What a program may keep from one speculative decoding step to the next (host only)."""
+"""What a program may keep from one call to the next: workspaces, prepared stacks (host only)."""
 import ctypes
 import gc
 import random
@@ -69,5 +69,33 @@ def test_a_draft_stack_holds_its_tensors():
     d, a, c = stack._layers[0], stack._layers[1], stack._convs[0]
     assert [d.k, d.v, d.beta, d.g, d.state[0], a.k_cache[0], a.v_cache[0], c.state, c.x] == addresses
     del stack, d, a, c
+    gc.collect()
+    assert all(r() is None for r in refs)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="host tensors stand in for device tensors")
+def test_a_stack_update_holds_its_tensors():
+    bf = torch.bfloat16
+    ctx = tu.Context(20, device="cpu")
+    ctx.set_metadata([(0, 10)], 50)
+    delta = tu.LayerIO(tu.TU_LAYER_DELTA, torch.zeros(3, 2, 64, dtype=bf), torch.zeros(3, 2, 64, dtype=bf),
+                       torch.zeros(3, 4, 64, dtype=bf), torch.zeros(3, 4, 64), state=[torch.zeros(4, 64, 64)],
+                       beta=torch.zeros(3, 4), g=torch.zeros(3, 4))
+    attn = tu.LayerIO(tu.TU_LAYER_ATTN, torch.zeros(3, 4, 64, dtype=bf), torch.zeros(3, 2, 64, dtype=bf),
+                      torch.zeros(3, 2, 64, dtype=bf), torch.zeros(3, 4, 64), k_cache=[torch.zeros(20, 2, 64, dtype=bf)],
+                      v_cache=[torch.zeros(20, 2, 64, dtype=bf)])
+    index = [torch.zeros(20, dtype=torch.int32)]
+    up = tu.StackUpdate([ctx], [[[2, 4]]], [3], [delta, attn], tu.attn_params(4, 2, 64), tu.delta_params(2, 4, 64, 64, 16),
+                        src_index=index)
+    given = [delta.q, delta.k, delta.v, delta.out, delta.beta, delta.g, delta.state[0], attn.q, attn.k, attn.v, attn.out,
+             attn.k_cache[0], attn.v_cache[0], index[0]]
+    refs = [weakref.ref(t) for t in given]
+    del given
+    for L in (delta, attn):
+        L.q = L.k = L.v = L.out = L.beta = L.g = None
+    delta.state[0], attn.k_cache[0], attn.v_cache[0], index[0] = None, None, None, None
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    del up
     gc.collect()
     assert all(r() is None for r in refs)
