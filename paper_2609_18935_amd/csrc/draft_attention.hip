@@ -48,8 +48,10 @@ constexpr int kUnit = kDraftUnit;
 // 2^(kLift + 14) below the largest still has all of f16's bits, and what P loses below is at most
 // 2^-(kLift + 25) of the largest. (Without kLift, many keys 17 e-folds below one whose value is small
 // came out as zeros. 13 and 2 move the reference more often: 64 nodes over 65,536 rows 84.2 -> 86.2 us.)
-constexpr float kLift = 11.f, kRise = 4.f;
-static_assert(kLift + kRise < 16.f, "P within f16");
+// Near kHuge and beyond, where roundings of the score and the reference reach whole units, it moves at smaller
+// rises, and is the largest score itself.
+constexpr float kLift = 11.f, kRise = 4.f, kHuge = 0x1p22f;
+static_assert(kLift + kRise < 15.5f, "P within f16, with the roundings below kHuge");
 constexpr int kLgkmWait0 = 15 | (7 << 4) | (0 << 8) | (3 << 14);
 
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
@@ -382,8 +384,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx),
                                                      __builtin_bit_cast(uint32_t, mx), false, false);
     mx = fmaxf(__builtin_bit_cast(float, (uint32_t)sw[0]), __builtin_bit_cast(float, (uint32_t)sw[1])) * c2;
-    if (__any(mx - kLift > m_run + kRise)) {
-      const float m_new = fmaxf(m_run, mx - kLift);
+    if (__any(mx - m_run > __builtin_fmaf(fabsf(mx), -2.f / kHuge, kLift + kRise))) {
+      const float m_new = fmaxf(m_run, fabsf(mx) < kHuge ? mx - kLift : mx);
       const float alpha = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;

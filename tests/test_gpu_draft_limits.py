@@ -60,6 +60,25 @@ def test_attention_beside_a_sink(hq, hkv, D, rows, splits, gap):
     assert tu.workspace_faults(ws) == 0
 
 
+@pytest.mark.parametrize("hq,hkv,D", [(16, 2, 256), (8, 2, 128), (16, 4, 64)])
+@pytest.mark.parametrize("exponent", [10, 12, 13, 14, 15])
+@pytest.mark.parametrize("splits", [1, 4])
+def test_attention_of_scores_of_millions(hq, hkv, D, exponent, splits):
+    """Scores up to 2^27 that rise from key to key by far more than any rounding: the last cached key takes all."""
+    rows, n, rng = 300, 3, np.random.default_rng(exponent)
+    k, v = torch.zeros(rows + n, hkv, D, dtype=torch.bfloat16), bf16(rng, rows + n, hkv, D)
+    q = torch.zeros(n, hq, D, dtype=torch.bfloat16)
+    q[..., 0] = 2.0 ** exponent
+    k[:rows, :, 0] = ((1 + torch.arange(rows) % 128 / 128) * 2.0 ** (exponent + torch.arange(rows) // 128 - 2)).to(torch.bfloat16)[:, None]
+    out = torch.full((n, hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    tu.draft_attention(_ctx(rows, n), dev(k), dev(v), tu.attn_params(hq, hkv, D, kv_splits=splits), tu.Draft([-1, 0, 0]), dev(q), out)
+    want = f64(v)[rows - 1].repeat(hq // hkv, axis=0)[None].repeat(n, axis=0)
+    steps = np.diff(f64(k)[:rows, 0, 0]) * 2.0 ** exponent * D ** -0.5
+    assert (steps > 0).all() and steps[-1] > 500       # exp(-500) is nothing
+    # P and the partial output in f16, the sum of P in fp32, the output in bf16
+    assert worst(out, want, (BF16 + 2 * F16 + 4 * F32) * np.abs(want)) <= 1
+
+
 @pytest.mark.parametrize("hq,hkv,D,rows,n,splits", [(16, 2, 256, 0, 1, 0), (16, 2, 256, 40, 9, 1), (16, 2, 256, 900, 9, 0),
                                                     (8, 2, 128, 40, 9, 1), (8, 2, 128, 500, 9, 4), (16, 4, 64, 0, 1, 0),
                                                     (16, 4, 64, 300, 9, 1)])
