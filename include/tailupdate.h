@@ -551,9 +551,12 @@ int draft_append(const tu_seq* seq, void* k_cache, void* v_cache, const tu_attn_
  * rows len + j of its ancestors j and itself (their keys and values written by
  * draft_append).
  *  q_hat: device bf16 [n][n_q_heads][head_dim], normed and rotated;
- *  out:   device bf16 [n][n_q_heads][head_dim], what the output projection reads (softmax
- *         and sums in fp32, one rounding to bf16 at the end).
- * Values are read as f16 (see the input range above; TU_FAULT_RANGE for finite magnitudes of
+ *  out:   device bf16 [n][n_q_heads][head_dim], what the output projection reads.
+ * Scores, the softmax's maximum and sum and the sums of p v are fp32. Before the rounding to bf16 of
+ * an output, p is rounded to f16 (2^-11 of it, at most 2^-36 of the largest p of the row
+ * where that is more), and so is each partial output of a split key range (2^-11 of it, or 2^-25).
+ * A query without a finite score (an infinite or NaN element) gives NaN.
+ * Values are read as f16 (see the input range above; TU_FAULT_RANGE for magnitudes of
  * 2^16 or more). A node's key or value that is not finite (or beyond f16) reaches only the nodes that see it. The
  * result does not depend on rows behind the last node. p->kv_splits as in
  * tail_prefill_attention (more where a split's rows would span 2 GB).
