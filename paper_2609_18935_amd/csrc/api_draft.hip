@@ -90,13 +90,14 @@ void norm_record(const tu_attn_params* p, const tu_qk_norm* norm, int64_t T, Nor
 
 // Splits of the key range and rows of a workgroup (in waves of 32) of the attention, by their estimated time.
 // A workgroup holds a CU. In microseconds, as fitted to launches over 0 to 50,000 rows, trees of 1 to 128
-// nodes and four head layouts (the choice is within 1 % of the best measured one in the mean): a stage takes 1.0 +
+// nodes and four head layouts (the choice is 1.6 % behind the best of the forced ones in the mean, 13 % at worst: 128
+// nodes over 12,000 rows of 8 heads of 128): a stage takes 1.0 +
 // 0.03 a wave with rows (0.7 of that with head_dim 64, whose stages are half as long), a wave's queries and outputs 0.1,
 // those of a second wave on a SIMD 0.6, the join's launch 2.8 and its partial outputs a microsecond for 2 MB on
 // their way through memory; what the tiles read again costs one for 40 MB. So short contexts take one split and small tiles (16 + 2 heads of 256, 64
-// nodes over 40 rows: 9.9 us in 16 tiles of one wave, 14.4 in two of eight, 15.1 with four splits), long ones
-// one tile and a split for every CU (64 nodes over 24,000 rows: 41.4 us in two tiles of eight waves, 43.5 in
-// four of four; 24 nodes over 3,000: 14.2 in three tiles of two and 32 splits, 17.3 in one of six, 21.4 with 95 splits).
+// nodes over 40 rows: 9.9 us in 16 tiles of one wave, 14.5 in two of eight, 15.0 with four splits), long ones
+// one tile and a split for every CU (64 nodes over 24,000 rows: 40.6 us in two tiles of eight waves, 42.8 in
+// four of four; 24 nodes over 3,000: 14.2 in three tiles of two and 32 splits, as chosen, 16.2 in one of six, 20.6 with 95 splits).
 struct DraftPlan {
   int splits;
   int tile_waves;

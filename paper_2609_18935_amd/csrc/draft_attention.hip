@@ -17,7 +17,8 @@
 //
 // The two waves of a SIMD take turns: while waves 0 - 3 run the matrix products of a stage (P V of
 // the stage before, then K Q^T), waves 4 - 7 run the softmax of theirs, and a barrier later the
-// other way round, so that the matrix core always has a wave to feed it.
+// other way round. With rows for four waves or fewer, waves 4 - 7 only load, and products and softmax of a
+// stage follow one another.
 //
 // A row of D dims lies in LDS as D / 8 chunks of 16 bytes, permuted within the row so that the
 // rows read together fall into different banks: chunk c of K row r at c ^ (r mod 16), of V row r at
@@ -27,13 +28,15 @@
 // The tree only matters to the units of 32 keys that reach past row len: there each lane shifts its
 // node's mask to the unit and drops the keys whose bit is clear.
 //
-// Measured with heads 16 / 2 of 256: 64 nodes over 65,536 rows 70 us (135 MB, 69 GFLOP) + 8 for the
-// join (34 MB of partial outputs), about 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an 8192^3 bf16 matrix product sustains here;
-// the matrix cores are busy in 53 % of all cycles, 62 % within the loop): bound by the matrix cores at the clock
-// that the power allows. One node over 32,768 rows 15 us + 3: HBM (67 MB, 4.4 TB/s). 24
-// nodes over 11,907 rows 14 + 4 (two tiles of 96 rows, 64 splits): Q (48 KB a workgroup) and its partial
-// outputs (48 KB) cost half as much as the six stages between them. One node over 300 rows 8.4 us with the
-// join, 24 9.6, without cached rows 6.3: latency.
+// Measured with heads 16 / 2 of 256: 64 nodes over 65,536 rows 70 us at the least (135 MB, 69 GFLOP) + 8 for the
+// join (34 MB of partial outputs), 78 to 86 together in a long run; 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an
+// 8192^3 bf16 matrix product sustains here). The matrix cores are busy in 65,600 of 124,000 cycles (53 %), the LDS in
+// 41,100; fragments are read only three ahead of the products, but which waits make up the rest is not known. One node over 32,768 rows 15 us + 3: HBM (67 MB, 4.4 TB/s). 24 nodes over
+// 11,907 rows 14 + 4 (two tiles of 96 rows, 64 splits; 20 together where the cache comes from HBM): three waves' work a
+// workgroup, each stage's products and softmax one behind the other, and Q (48 KB a workgroup) and its partial outputs (48
+// KB) half as long as the six stages between them. One node over 300 rows 8.5 us with the join, 24 9.6, without cached
+// rows 6.3: latency. Heads of 64 (32 / 8 of 128): 24 nodes over 24,000 rows 14.2 us, of which the 25 MB of K and V are 4.9
+// (27.7; 98 MB, 19.5): one workgroup a CU, as with the wider heads, though registers or LDS of two would nearly fit.
 #include "attention_tile.h"
 #include "draft.h"
 

@@ -4,7 +4,7 @@
 // Convolution. A thread takes 8 channels of one node: the rows under the taps are the node's
 // and those of its ancestors, then the carried ones; products are summed in fp32 in tap order
 // and rounded once to bf16. Bound by latency and issue: a layer's rows and weights (a few MB)
-// stay in L2. Measured, 8,192 channels of width 4: one node 3.0 us, 64 3.7, 128 4.6.
+// stay in L2. Measured in a graph of such calls, 8,192 channels of width 4: one node 3.1 us, 64 3.4, 128 4.2.
 //
 // Delta rule. Evaluated token by token a tree needs a state (d x d fp32) per node; in the
 // WY form it needs the carried state once. With D_ij = gamma_i / gamma_j where j is an ancestor
@@ -29,8 +29,8 @@
 //
 // Bound by latency, not by its bytes (2 to 6 MB) or products: one trip to memory for all operands, then
 // five dependent phases (gates along the paths, products with S and between nodes, inverses, the
-// solve block by block, outputs) with one wave a SIMD. Measured, 16 key and 32 value heads of 128: 1 node
-// 4.6 us, 7 5.0, 16 5.4, 32 6.4, 64 8.2, 65 12.1, 128 14.9.
+// solve block by block, outputs) with one wave a SIMD. Measured in a graph of such calls, 16 key and 32 value heads
+// of 128: 1 node 4.7 us, 7 5.0, 16 5.3, 32 6.3, 64 8.1 (7.4 a call launched by itself), 65 11.9, 128 14.7.
 //
 // A node whose inputs are not finite must not reach nodes of other paths (0 x NaN in a product
 // of blocks): it is left out, and its outputs and its descendants' set to NaN.

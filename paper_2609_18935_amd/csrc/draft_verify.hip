@@ -14,9 +14,10 @@
 // the few workgroups fit the chip many times over) and adds all of them up in one order. The
 // workgroup whose slice holds the drawn token finds it. Bound by latency: the odds (two
 // dependent loads), the rows of a node (a load; a megabyte, kept in registers over its passes)
-// and one exchange a pass; and by fetching code that runs once, so it is kept small. Measured over a
-// vocabulary of 131,072: 7.5 us for one node, 7.9 for a chain of six, 11.5 for 64 nodes with several
-// rejections (k_draft_clear 1.4 of it), 16.6 without proposals.
+// and one exchange a pass; and by fetching code that runs once, so it is kept small. Measured in a graph of such
+// calls over a vocabulary of 131,072: 7.9 us for one node, 8.5 for a chain of six, 10 to 11 for 64 nodes with
+// several rejections (k_draft_clear 1.4 of it), 12 to 14 without proposals (more rejections; each sums its row again,
+// though a point mass only takes p(x) from F).
 #include <algorithm>
 
 #include "draft.h"

@@ -17,7 +17,7 @@
 // and what other kernels left in the caches stays). Outputs are not written so: the attention behind
 // finds them in the caches (4,096 tokens: 292 us for both; 312 with streamed outputs).
 // Measured, 16 + 2 heads of 256, rotated whole: 8,191 tokens 31.5 us (151 MB, 4.8 TB/s, a copy
-// 5.06), 1,000 8.7, one 3.4 (latency: the launch, one trip to memory, one rotation).
+// 5.06), 1,000 7.6, one 3.4 (latency: the launch, one trip to memory, one rotation).
 #include "draft.h"
 #include "tailupdate.h"
 
