@@ -94,7 +94,7 @@ struct DraftDeltaArgs {
 constexpr int kDrawThreads = 512;
 constexpr int kDrawPer = 8;       // consecutive row elements of a thread, in registers
 constexpr int kDrawMaxBlocks = 64;
-constexpr int kDrawPolls = 1 << 20;   // of a wait for another workgroup: many milliseconds
+constexpr int kDrawPolls = 1 << 20;   // of a wait for the other workgroups, each a trip to memory
 struct DraftVerifyArgs {
   const int32_t* tokens;
   const float* target;

@@ -30,13 +30,15 @@
 //
 // Measured with heads 16 / 2 of 256: 64 nodes over 65,536 rows 70 us at the least (135 MB, 69 GFLOP) + 8 for the
 // join (34 MB of partial outputs), 78 to 86 together in a long run; 2.1 us a stage (1.17 PFLOP/s, 0.91 of what an
-// 8192^3 bf16 matrix product sustains here). The matrix cores are busy in 65,600 of 124,000 cycles (53 %), the LDS in
-// 41,100; fragments are read only three ahead of the products, but which waits make up the rest is not known. One node over 32,768 rows 15 us + 3: HBM (67 MB, 4.4 TB/s). 24 nodes over
-// 11,907 rows 14 + 4 (two tiles of 96 rows, 64 splits; 20 together where the cache comes from HBM): three waves' work a
-// workgroup, each stage's products and softmax one behind the other, and Q (48 KB a workgroup) and its partial outputs (48
-// KB) half as long as the six stages between them. One node over 300 rows 8.5 us with the join, 24 9.6, without cached
-// rows 6.3: latency. Heads of 64 (32 / 8 of 128): 24 nodes over 24,000 rows 14.2 us, of which the 25 MB of K and V are 4.9
-// (27.7; 98 MB, 19.5): one workgroup a CU, as with the wider heads, though registers or LDS of two would nearly fit.
+// 8192^3 bf16 matrix product sustains here). The matrix cores are busy in 65,600 of 124,000 cycles (53 %), the LDS
+// in 41,100; fragments are read only three ahead of the products, but which waits make up the rest is not known.
+// One node over 32,768 rows 15 us + 3: HBM (67 MB, 4.4 TB/s). 24 nodes over 11,907 rows 14 + 4 (two tiles of 96
+// rows, 64 splits; 20 together where the cache comes from HBM): three waves' work a workgroup, each stage's
+// products and softmax one behind the other, and Q (48 KB a workgroup) and its partial outputs (48 KB) half as long
+// as the six stages between them. One node over 300 rows 8.5 us with the join, 24 9.6, without cached rows 6.3:
+// latency. 24 nodes over 24,000 rows: heads 16 / 4 of 64 14.2 us (25 MB of K and V, 4.9 us of a copy), heads 32 / 8
+// of 128 27.7 (98 MB, 19.5). One workgroup a CU there too: that of heads of 64 takes 72 KB of LDS and 137 registers
+// a lane, 9 more than two workgroups would have.
 #include "attention_tile.h"
 #include "draft.h"
 

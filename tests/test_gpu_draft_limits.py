@@ -115,9 +115,14 @@ def test_a_workspace_kept_over_steps_of_other_sizes():
 
 
 def _record(name):
-    """The launch record `name` as the library's header declares it."""
-    with open(os.path.join(os.path.dirname(tu.__file__), "csrc", "draft.h")) as f:
-        body = re.search(r"struct %s \{\n(.*?)\n\};" % name, f.read(), re.S).group(1)
+    """The launch record `name` as the library's headers declare it."""
+    src = ""
+    for header in ("common.h", "draft.h"):
+        with open(os.path.join(os.path.dirname(tu.__file__), "csrc", header)) as f:
+            src += f.read()
+    body = re.search(r"struct %s \{\n(.*?)\n\};" % name, src, re.S).group(1)
+    assert "constexpr int kMaxDraft = 128;" in src and "struct DraftMasks {\n  uint64_t m[kMaxDraft][2];\n};" in src
+    assert "struct CallStatus {\n  unsigned long long* word;\n  uint32_t* last;\n  uint32_t call;\n  uint32_t pad;\n};" in src
 
     class CallStatus(ctypes.Structure):
         _fields_ = [("word", ctypes.c_void_p), ("last", ctypes.c_void_p), ("call", ctypes.c_uint32)]
